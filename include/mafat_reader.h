@@ -1,0 +1,57 @@
+/*
+ * mafat_reader.h -- C ABI of the operators of a reader: a decoder whose
+ * tokens, of many requests at once, read the feature maps that a plan's
+ * network (mafat.h) leaves on the device.  They are not part of the paper's
+ * method; they consume its output where it lies.
+ *
+ *   mafat_add_rms_norm     residual addition and root-mean-square norm, into
+ *                          float32, bfloat16 or 8 bits with a scale per row
+ *
+ * Conventions of mafat.h hold: device buffers are the caller's, run functions
+ * enqueue kernels on the given stream and return, no device memory is
+ * allocated, nothing synchronises, no exception leaves, equal calls give
+ * equal bits.  Strides are in elements and may leave gaps; the last axis is
+ * contiguous.  Pointers need the alignment of their elements only; rows of
+ * 16-byte alignment run fastest.  Sizes of zero rows are valid and enqueue
+ * nothing.
+ *
+ * MAFAT_F8 is the 8-bit float of 4 exponent and 3 mantissa bits with largest
+ * value 448 and no infinities (OCP e4m3).
+ */
+#ifndef MAFAT_READER_H
+#define MAFAT_READER_H
+
+#include "mafat.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { MAFAT_F8 = 2 };
+
+/* h = x + residual, rounded to dtype and written to sum; without a residual
+ * (residual and sum NULL) h = x.  Then, per row,
+ *   y = h * (mean(h^2) + eps)^(-1/2) * gain
+ * with the mean over cols in float32.  out_dtype MAFAT_F8: y_scale[row] =
+ * max |y| / 448 and y holds y / y_scale rounded to nearest even; a row whose
+ * largest magnitude is below 2^-100 (one of zeros) gets scale 1.  A row with
+ * a NaN gets NaN outputs and a NaN scale.
+ *   x, residual, sum   rows x cols in dtype (MAFAT_F32 or MAFAT_BF16)
+ *   gain               float32[cols], or NULL (ones)
+ *   y                  rows x cols in out_dtype (MAFAT_F32, MAFAT_BF16, MAFAT_F8)
+ *   y_scale            float32[rows] for MAFAT_F8, else NULL
+ * sum may be x or residual itself (with its stride); otherwise outputs may
+ * not overlap inputs or each other.  Errors: EINVAL (null or misaligned
+ * pointer, negative size, cols < 1, stride below cols, one of residual and
+ * sum without the other, a scale pointer that does not match out_dtype,
+ * overlap, eps negative or not finite), EUNSUPPORTED (dtype; rows or cols of
+ * 2^31 or more), EHIP. */
+int mafat_add_rms_norm(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t x_stride,
+                       const void* residual, int64_t residual_stride, const float* gain, float eps,
+                       void* sum, int64_t sum_stride, int32_t out_dtype, void* y, int64_t y_stride,
+                       float* y_scale, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif
