@@ -6,6 +6,8 @@
  *
  *   mafat_add_rms_norm     residual addition and root-mean-square norm, into
  *                          float32, bfloat16 or 8 bits with a scale per row
+ *   mafat_linear           projection of 8-bit rows by 8-bit weights, with
+ *                          low-rank adapters of the requests beside it
  *
  * Conventions of mafat.h hold: device buffers are the caller's, run functions
  * enqueue kernels on the given stream and return, no device memory is
@@ -13,7 +15,9 @@
  * equal bits.  Strides are in elements and may leave gaps; the last axis is
  * contiguous.  Pointers need the alignment of their elements only; rows of
  * 16-byte alignment run fastest.  Sizes of zero rows are valid and enqueue
- * nothing.
+ * nothing.  Integer inputs on the device (adapter numbers) are not read on
+ * the host: out-of-range values are clamped or ignored as stated and never
+ * lead outside a buffer.
  *
  * MAFAT_F8 is the 8-bit float of 4 exponent and 3 mantissa bits with largest
  * value 448 and no infinities (OCP e4m3).
@@ -50,6 +54,43 @@ int mafat_add_rms_norm(int64_t rows, int64_t cols, int32_t dtype, const void* x,
                        const void* residual, int64_t residual_stride, const float* gain, float eps,
                        void* sum, int64_t sum_stride, int32_t out_dtype, void* y, int64_t y_stride,
                        float* y_scale, void* stream);
+
+/* Low-rank adapters of mafat_linear: adapter i adds, to the rows that name
+ * it, factor[i] * b[i] (a[i] x).
+ *   a       bfloat16 [count][rank][in_cols], contiguous
+ *   b       bfloat16 [count][out_cols][rank], contiguous
+ *   factor  float32 [count], or NULL (ones)
+ *   of_row  int32 [rows]: each row's adapter; any value outside
+ *           [0, count) is none
+ * All on the device; 1 <= rank <= 128. */
+typedef struct {
+  int32_t count, rank;
+  const void* a;
+  const void* b;
+  const float* factor;
+  const int32_t* of_row;
+} mafat_adapters;
+
+/* y[i][j] = x_scale[i] * w_scale[j] * sum_k x[i][k] w[j][k] + bias[j], plus
+ * the row's adapter on the values x stands for, in bfloat16.
+ *   x        8 bits [rows][in_cols], w 8 bits [out_cols][in_cols]
+ *   x_scale  float32[rows], w_scale float32[out_cols]
+ *   bias     float32[out_cols], or NULL
+ *   adapters a host struct, read during the call, or NULL
+ *   workspace  mafat_linear_workspace bytes, 256-byte aligned (NULL if 0)
+ * Sums are float32.  The 8-bit matrix instructions align the products of a
+ * step before they add them: a sum is within about 2e-5 of the exact one,
+ * relative to the root of the sum of its squared products.  Errors: EINVAL
+ * (null or misaligned pointer, negative size, in_cols or out_cols < 1,
+ * stride below the row length, bad adapters, y overlapping an input),
+ * EWORKSPACE, EUNSUPPORTED (rank > 128, sizes or a stride of 2^22 or more
+ * columns, 2^31 or more rows), EHIP. */
+int mafat_linear_workspace(int64_t rows, int64_t in_cols, int64_t out_cols,
+                           const mafat_adapters* adapters, size_t* bytes);
+int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, const void* x, int64_t x_stride,
+                 const float* x_scale, const void* w, int64_t w_stride, const float* w_scale,
+                 const float* bias, const mafat_adapters* adapters, void* y, int64_t y_stride,
+                 void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

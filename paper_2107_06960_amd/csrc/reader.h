@@ -25,4 +25,25 @@ struct NormArgs {
 };
 hipError_t launch_norm(int dtype, int out_dtype, const NormArgs& a, hipStream_t stream);
 
+
+struct LinearArgs {
+  const unsigned char* x;
+  const unsigned char* w;
+  const float* x_scale;
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  // adapters (count 0: none); u: float32 [rows][rank], factor * x_scale * (a x)
+  const uint16_t* a;
+  const uint16_t* b;
+  const float* factor;
+  const int32_t* of_row;
+  float* u;
+  int64_t x_stride, w_stride, y_stride;
+  int64_t rows;
+  int32_t in_cols, out_cols;
+  int32_t count, rank;
+};
+hipError_t launch_linear(const LinearArgs& a, hipStream_t stream);
+
 }  // namespace mafat

@@ -50,3 +50,44 @@ def test_norm_refusals(change, status):
 
 def test_norm_of_no_rows_is_valid():
     assert O.lib().mafat_add_rms_norm(*dict(NORM, rows=0).values()) == 0
+
+
+def _adapters(**change):
+    return O.mafat_adapters(**dict(dict(count=3, rank=8, a=C, b=C + (1 << 24), factor=C + (1 << 25), of_row=C + (1 << 26)),
+                                   **change))
+
+
+LINEAR = dict(rows=20, in_cols=64, out_cols=48, x=A, x_stride=64, x_scale=A + (1 << 30), w=B, w_stride=64,
+              w_scale=B + (1 << 30), bias=B + (1 << 31), adapters=None, y=D, y_stride=48, workspace=E, ws_bytes=1024,
+              stream=None)
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(rows=-1), EINVAL), (dict(in_cols=0), EINVAL), (dict(out_cols=0), EINVAL), (dict(rows=1 << 31), EUNSUPPORTED),
+    (dict(in_cols=1 << 22, x_stride=1 << 22, w_stride=1 << 22), EUNSUPPORTED), (dict(out_cols=1 << 22), EUNSUPPORTED),
+    (dict(x_stride=63), EINVAL), (dict(w_stride=0), EINVAL), (dict(y_stride=47), EINVAL),
+    (dict(x_stride=1 << 22), EUNSUPPORTED), (dict(w_stride=1 << 22), EUNSUPPORTED), (dict(y_stride=1 << 31), EUNSUPPORTED),
+    (dict(x=None), EINVAL), (dict(w=None), EINVAL), (dict(x_scale=None), EINVAL), (dict(w_scale=None), EINVAL),
+    (dict(y=None), EINVAL), (dict(y=D + 1), EINVAL), (dict(x_scale=A + (1 << 30) + 2), EINVAL),
+    (dict(bias=B + (1 << 31) + 1), EINVAL),
+    (dict(y=A), EINVAL), (dict(y=B + 64 * 47), EINVAL), (dict(y=B + (1 << 31)), EINVAL),
+    (dict(adapters=_adapters(count=0)), EINVAL), (dict(adapters=_adapters(rank=0)), EINVAL),
+    (dict(adapters=_adapters(rank=129)), EUNSUPPORTED), (dict(adapters=_adapters(a=None)), EINVAL),
+    (dict(adapters=_adapters(b=None)), EINVAL), (dict(adapters=_adapters(of_row=None)), EINVAL),
+    (dict(adapters=_adapters(of_row=C + 2)), EINVAL), (dict(adapters=_adapters(a=C + 1)), EINVAL),
+    (dict(adapters=_adapters(), ws_bytes=639), M.MAFAT_EWORKSPACE), (dict(adapters=_adapters(), workspace=None), EINVAL),
+    (dict(adapters=_adapters(), workspace=E + 128), EINVAL), (dict(adapters=_adapters(), workspace=D), EINVAL),
+    (dict(adapters=_adapters(), workspace=A), EINVAL), (dict(adapters=_adapters(), y=C), EINVAL),
+])
+def test_linear_refusals(change, status):
+    rc = O.lib().mafat_linear(*dict(LINEAR, **change).values())
+    assert rc == status, O.lib().mafat_last_error()
+    assert O.lib().mafat_last_error()
+
+
+def test_linear_workspace_and_no_rows():
+    assert O.mafat_linear_workspace(20, 64, 48) == 0
+    assert O.mafat_linear_workspace(20, 64, 48, _adapters()) >= 20 * 8 * 4
+    assert O.lib().mafat_linear_workspace(20, 64, 48, None, None) == EINVAL
+    assert O.lib().mafat_linear(*dict(LINEAR, rows=0).values()) == 0
+    assert O.lib().mafat_linear(*dict(LINEAR, rows=0, adapters=_adapters(), ws_bytes=0, workspace=None).values()) == 0
