@@ -8,6 +8,8 @@
  *                          float32, bfloat16 or 8 bits with a scale per row
  *   mafat_linear           projection of 8-bit rows by 8-bit weights, with
  *                          low-rank adapters of the requests beside it
+ *   mafat_cross_attention  attention of the requests' tokens to the positions
+ *                          of the frames they are about
  *
  * Conventions of mafat.h hold: device buffers are the caller's, run functions
  * enqueue kernels on the given stream and return, no device memory is
@@ -15,9 +17,9 @@
  * equal bits.  Strides are in elements and may leave gaps; the last axis is
  * contiguous.  Pointers need the alignment of their elements only; rows of
  * 16-byte alignment run fastest.  Sizes of zero rows are valid and enqueue
- * nothing.  Integer inputs on the device (adapter numbers) are not read on
- * the host: out-of-range values are clamped or ignored as stated and never
- * lead outside a buffer.
+ * nothing.  Integer inputs on the device (lengths, offsets, adapter
+ * numbers) are not read on the host: out-of-range values are clamped or
+ * ignored as stated and never lead outside a buffer.
  *
  * MAFAT_F8 is the 8-bit float of 4 exponent and 3 mantissa bits with largest
  * value 448 and no infinities (OCP e4m3).
@@ -91,6 +93,54 @@ int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, const void* x,
                  const float* x_scale, const void* w, int64_t w_stride, const float* w_scale,
                  const float* bias, const mafat_adapters* adapters, void* y, int64_t y_stride,
                  void* workspace, size_t ws_bytes, void* stream);
+
+/* Sizes and strides of mafat_cross_attention.  Query rows are those of all
+ * requests about all frames, frame by frame; every query head h reads the
+ * keys and values of head h / (q_heads / kv_heads). */
+typedef struct {
+  int32_t dtype;              /* MAFAT_F32 or MAFAT_BF16: q, k, v and y */
+  int32_t frames;             /* key/value sequences */
+  int64_t rows;               /* query rows of all frames together */
+  int64_t positions;          /* positions of a frame's k and v */
+  int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
+  int32_t head_dim;           /* 1 .. 256, of keys and of values */
+  float scale;                /* of q . k */
+  int64_t q_row, q_head;      /* strides of q */
+  int64_t k_frame, k_pos, k_head;
+  int64_t v_frame, v_pos, v_head;
+  int64_t y_row, y_head;
+  int64_t mask_row;           /* bytes between rows of the mask */
+  int32_t mask_by_row;        /* 0: a mask row per frame; 1: per query row */
+} mafat_cross;
+
+/* For every query row i of frame f and head h, over the frame's valid
+ * positions s (s < k_lengths[f], and allowed by the mask):
+ *   p_s = softmax_s(scale * q[i][h] . k[f][s][h'])
+ *   y[i][h] = sum_s p_s v[f][s][h'],  lse[i][h] = log sum_s exp(scale * ...)
+ * A row that no position is valid for gets y = 0 and lse = -infinity.  Keys
+ * and values of positions that are not valid for any row of a frame by its
+ * length or its mask may hold anything, NaN included.
+ *   q_offsets  int32[frames + 1], not decreasing, each clamped to [0, rows]:
+ *              frame f's rows are [q_offsets[f], q_offsets[f + 1]); rows that
+ *              no frame has are not written.  (Offsets that decrease leave it
+ *              open which rows are computed.)  NULL: rows / frames each (rows
+ *              must divide)
+ *   k_lengths  int32[frames], clamped to [0, positions]; NULL: positions
+ *   mask       bytes, nonzero where a position may be read; [frames or
+ *              rows][positions] by mask_by_row; or NULL
+ *   y          [rows][q_heads][head_dim] in dtype;  lse float32 [rows][q_heads]
+ *              contiguous, natural logarithm, or NULL
+ *   workspace  mafat_cross_workspace bytes, 256-byte aligned (NULL if 0)
+ * Softmax statistics and sums are float32; bfloat16 probabilities enter the
+ * second product rounded to bfloat16, each by its own size.  Errors: EINVAL
+ * (null or misaligned pointer, bad size or stride, rows not divisible without
+ * q_offsets, scale not finite, y overlapping an input), EWORKSPACE,
+ * EUNSUPPORTED (dtype, head_dim > 256, sizes of 2^31 or more, strides of 2^31
+ * bytes or more), EHIP. */
+int mafat_cross_workspace(const mafat_cross* c, size_t* bytes);
+int mafat_cross_attention(const mafat_cross* c, const void* q, const void* k, const void* v,
+                          const int32_t* q_offsets, const int32_t* k_lengths, const unsigned char* mask,
+                          void* y, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,7 +1,9 @@
 // reader.cpp -- C ABI of the reader's operators (include/mafat_reader.h):
 // checks of the arguments, choice of the kernels' work split, launches.
 #include <cmath>
+#include <initializer_list>
 #include <string>
+#include <utility>
 
 #include "mafat_internal.h"
 #include "reader.h"
@@ -26,6 +28,9 @@ struct Span {
   int64_t rows;
   int64_t width, pitch;
 };
+
+// Whether n rows of a stride have an extent that byte arithmetic can hold.
+bool fits(int64_t n, int64_t stride) { return n < 1 || stride < (int64_t{1} << 58) / n; }
 
 // Whether two tensors share a byte.  Tensors of one pitch may lie side by side
 // in the rows of one buffer; others count as overlapping if their extents do.
@@ -60,6 +65,45 @@ int check_linear(int64_t rows, int64_t in_cols, int64_t out_cols, const mafat_ad
     *bytes = (static_cast<size_t>(rows) * ad->rank * sizeof(float) + 255) & ~size_t{255};
   }
   return MAFAT_OK;
+}
+
+// The sizes and strides of an attention call; the workspace holds the parts
+// that the splits of the positions are joined from.
+int check_cross(const mafat_cross* c, size_t* bytes) {
+  if (!c) return fail(MAFAT_EINVAL, "c is NULL");
+  if (c->dtype != MAFAT_F32 && c->dtype != MAFAT_BF16) return fail(MAFAT_EUNSUPPORTED, "dtype must be F32 or BF16");
+  if (c->frames < 1 || c->rows < 0 || c->positions < 0) return fail(MAFAT_EINVAL, "frames must be >= 1, rows and positions >= 0");
+  if (c->kv_heads < 1 || c->q_heads < 1 || c->q_heads % c->kv_heads)
+    return fail(MAFAT_EINVAL, "q_heads must be a multiple of kv_heads");
+  if (c->head_dim < 1) return fail(MAFAT_EINVAL, "head_dim must be >= 1");
+  if (c->head_dim > 256) return fail(MAFAT_EUNSUPPORTED, "head_dim above 256");
+  if (!std::isfinite(c->scale)) return fail(MAFAT_EINVAL, "scale must be finite");
+  const int64_t d = c->head_dim;
+  if (c->q_head < d || c->k_head < d || c->v_head < d || c->y_head < d)
+    return fail(MAFAT_EINVAL, "a head stride is smaller than head_dim");
+  if (c->q_row < d || c->y_row < d || c->k_pos < d || c->v_pos < d || c->k_frame < d || c->v_frame < d || c->mask_row < 0)
+    return fail(MAFAT_EINVAL, "a row, position or frame stride is smaller than head_dim");
+  const int64_t most = kMax31 / (c->dtype == MAFAT_F32 ? 4 : 2);
+  if (c->rows >= kMax31 / c->q_heads || c->positions >= kMax31 || c->frames >= kMax31 / c->kv_heads || c->kv_heads > 65535)
+    return fail(MAFAT_EUNSUPPORTED, "rows * q_heads, positions or frames * kv_heads of 2^31 or more, or more than 65535 kv_heads");
+  if (c->q_row >= most || c->y_row >= most || c->k_pos >= most || c->v_pos >= most || c->q_head >= most || c->k_head >= most ||
+      c->v_head >= most || c->y_head >= most)
+    return fail(MAFAT_EUNSUPPORTED, "a row, position or head stride of 2^31 bytes or more");
+  if (!fits(c->rows, c->q_row) || !fits(c->rows, c->y_row) || !fits(c->positions, c->k_pos) || !fits(c->positions, c->v_pos) ||
+      !fits(c->frames, c->k_frame) || !fits(c->frames, c->v_frame) || !fits(c->mask_by_row ? c->rows : c->frames, c->mask_row))
+    return fail(MAFAT_EUNSUPPORTED, "an extent of 2^58 or more");
+  const int splits = cross_splits(*c);
+  *bytes = splits > 1 ? (static_cast<size_t>(splits) * static_cast<size_t>(c->rows) * c->q_heads * (c->head_dim + 2) * 4 + 255) & ~size_t{255}
+                      : 0;
+  return MAFAT_OK;
+}
+
+// Heads and rows as one extent (strides in any order).
+Span extent(const void* p, int64_t esz, int64_t d, std::initializer_list<std::pair<int64_t, int64_t>> axes) {
+  int64_t n = d;
+  for (const auto& a : axes)
+    if (a.first > 0) n += (a.first - 1) * a.second;
+  return {p, 1, n * esz, n * esz};
 }
 
 }  // namespace
@@ -132,7 +176,7 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
     if (rc != MAFAT_OK) return rc;
     if (x_stride < in_cols || w_stride < in_cols || y_stride < out_cols)
       return fail(MAFAT_EINVAL, "a stride is smaller than its row");
-    if (x_stride >= kMaxLinearCols || w_stride >= kMaxLinearCols || y_stride >= kMax31)
+    if (x_stride >= kMaxLinearCols || w_stride >= kMaxLinearCols || y_stride >= kMax31 || !fits(rows, y_stride))
       return fail(MAFAT_EUNSUPPORTED, "a stride of 2^22 or more (y: 2^31)");
     if (rows == 0) return static_cast<int>(MAFAT_OK);  // tensors of no rows may have no address
     if (!x || !x_scale || !w || !w_scale || !y) return fail(MAFAT_EINVAL, "x, w, their scales and y must be non-NULL");
@@ -151,7 +195,7 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
         return fail(MAFAT_EINVAL, "workspace must be non-NULL and 256-byte aligned");
       const int64_t an = 2 * static_cast<int64_t>(d.count) * d.rank * in_cols, bn = 2 * static_cast<int64_t>(d.count) * d.rank * out_cols;
       const Span su{workspace, 1, static_cast<int64_t>(need), static_cast<int64_t>(need)};
-      const Span others[] = {{d.a, 1, an, an}, {d.b, 1, bn, bn}, {d.factor, 1, 4 * d.count, 4 * d.count},
+      const Span others[] = {{d.a, 1, an, an}, {d.b, 1, bn, bn}, {d.factor, 1, 4 * int64_t{d.count}, 4 * int64_t{d.count}},
                              {d.of_row, 1, 4 * rows, 4 * rows}, {x, rows, in_cols, x_stride},
                              {w, out_cols, in_cols, w_stride}, {x_scale, 1, 4 * rows, 4 * rows},
                              {w_scale, 1, 4 * out_cols, 4 * out_cols}, {bias, 1, 4 * out_cols, 4 * out_cols}};
@@ -180,5 +224,67 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
     a.in_cols = static_cast<int32_t>(in_cols);
     a.out_cols = static_cast<int32_t>(out_cols);
     return launched(launch_linear(a, static_cast<hipStream_t>(stream)), "linear");
+  });
+}
+
+extern "C" int mafat_cross_workspace(const mafat_cross* c, size_t* bytes) {
+  return guarded([&] {
+    clear_error();
+    if (!bytes) return fail(MAFAT_EINVAL, "bytes is NULL");
+    return check_cross(c, bytes);
+  });
+}
+
+extern "C" int mafat_cross_attention(const mafat_cross* c, const void* q, const void* k, const void* v,
+                                     const int32_t* q_offsets, const int32_t* k_lengths, const unsigned char* mask,
+                                     void* y, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    clear_error();
+    size_t need = 0;
+    const int rc = check_cross(c, &need);
+    if (rc != MAFAT_OK) return rc;
+    if (c->rows == 0) return static_cast<int>(MAFAT_OK);  // tensors of no rows may have no address
+    if (!q_offsets && c->rows % c->frames) return fail(MAFAT_EINVAL, "rows must divide by frames without q_offsets");
+    if (!q || !y || (c->positions > 0 && (!k || !v))) return fail(MAFAT_EINVAL, "q, k, v and y must be non-NULL");
+    if (mask && c->mask_row < c->positions) return fail(MAFAT_EINVAL, "mask_row is smaller than positions");
+    const int64_t esz = static_cast<int64_t>(elt_size(c->dtype)), d = c->head_dim;
+    const size_t es = elt_size(c->dtype);
+    if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(y, es) || !aligned(q_offsets, 4) ||
+        !aligned(k_lengths, 4) || !aligned(lse, 4))
+      return fail(MAFAT_EINVAL, "a pointer is not aligned to its elements");
+    if (ws_bytes < need)
+      return fail(MAFAT_EWORKSPACE, "workspace " + std::to_string(ws_bytes) + " < " + std::to_string(need) + " bytes");
+    if (need > 0 && (!workspace || !aligned(workspace, 256)))
+      return fail(MAFAT_EINVAL, "workspace must be non-NULL and 256-byte aligned");
+    const int64_t mask_rows = c->mask_by_row ? c->rows : c->frames, lse_bytes = 4 * c->rows * c->q_heads;
+    const Span ins[] = {extent(q, esz, d, {{c->rows, c->q_row}, {c->q_heads, c->q_head}}),
+                        extent(c->positions ? k : nullptr, esz, d,
+                               {{c->frames, c->k_frame}, {c->positions, c->k_pos}, {c->kv_heads, c->k_head}}),
+                        extent(c->positions ? v : nullptr, esz, d,
+                               {{c->frames, c->v_frame}, {c->positions, c->v_pos}, {c->kv_heads, c->v_head}}),
+                        {q_offsets, 1, 4 * (c->frames + int64_t{1}), 4}, {k_lengths, 1, 4 * int64_t{c->frames}, 4},
+                        extent(c->positions ? mask : nullptr, 1, c->positions, {{mask_rows, c->mask_row}})};
+    const Span outs[] = {extent(y, esz, d, {{c->rows, c->y_row}, {c->q_heads, c->y_head}}),
+                         {lse, 1, lse_bytes, lse_bytes},
+                         {need ? workspace : nullptr, 1, static_cast<int64_t>(need), static_cast<int64_t>(need)}};
+    for (int i = 0; i < 3; ++i) {
+      for (const Span& s : ins)
+        if (overlap(outs[i], s)) return fail(MAFAT_EINVAL, "y, lse or the workspace overlaps an input");
+      for (int j = 0; j < i; ++j)
+        if (overlap(outs[i], outs[j])) return fail(MAFAT_EINVAL, "y, lse and the workspace overlap");
+    }
+    CrossArgs a{};
+    a.q = q; a.k = k; a.v = v; a.q_offsets = q_offsets; a.k_lengths = k_lengths;
+    a.mask = c->positions ? mask : nullptr;
+    a.y = y; a.lse = lse; a.part = static_cast<float*>(workspace);
+    a.q_row = c->q_row; a.q_head = c->q_head; a.k_frame = c->k_frame; a.k_pos = c->k_pos; a.k_head = c->k_head;
+    a.v_frame = c->v_frame; a.v_pos = c->v_pos; a.v_head = c->v_head; a.y_row = c->y_row; a.y_head = c->y_head;
+    a.mask_row = c->mask_row;
+    a.frames = c->frames; a.rows = static_cast<int32_t>(c->rows); a.positions = static_cast<int32_t>(c->positions);
+    a.q_heads = c->q_heads; a.kv_heads = c->kv_heads; a.group = c->q_heads / c->kv_heads; a.head_dim = c->head_dim;
+    a.mask_by_row = c->mask_by_row ? 1 : 0;
+    a.splits = cross_splits(*c);
+    a.scale = static_cast<float>(static_cast<double>(c->scale) * 1.4426950408889634);
+    return launched(launch_cross(c->dtype, a, static_cast<hipStream_t>(stream)), "cross attention");
   });
 }

@@ -46,4 +46,27 @@ struct LinearArgs {
 };
 hipError_t launch_linear(const LinearArgs& a, hipStream_t stream);
 
+struct CrossArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* q_offsets;
+  const int32_t* k_lengths;
+  const unsigned char* mask;
+  void* y;
+  float* lse;
+  // several splits of the positions: per split, row and head the sum of the
+  // values and, after all of these, largest score (base 2) and sum
+  float* part;
+  int64_t q_row, q_head, k_frame, k_pos, k_head, v_frame, v_pos, v_head, y_row, y_head, mask_row;
+  int32_t frames, rows, positions, q_heads, kv_heads, group, head_dim;
+  int32_t mask_by_row;
+  int32_t splits;
+  int32_t row_blocks;  // blocks of query rows, of all frames together (at most)
+  float scale;         // times log2(e): scores are in base 2
+};
+// Splits of the positions that a call's blocks are launched with.
+int cross_splits(const mafat_cross& c);
+hipError_t launch_cross(int dtype, const CrossArgs& a, hipStream_t stream);
+
 }  // namespace mafat

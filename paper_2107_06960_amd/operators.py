@@ -1,9 +1,10 @@
 """The operators of a reader (include/mafat_reader.h): a decoder whose tokens, of many requests at once, read the feature
 maps that a ``mafat.Network`` leaves on the device.
 
-``mafat_add_rms_norm`` and ``mafat_linear`` keep the C names and only marshal arguments (device pointers and sizes).
-``add_rms_norm`` and ``linear8`` take torch tensors on the GPU, check them, allocate what they return and run on the
-current stream of the tensors' device.  There is no fallback: every step runs in the library's HIP kernels.
+``mafat_add_rms_norm``, ``mafat_linear`` and ``mafat_cross_attention`` keep the C names and only marshal arguments
+(device pointers and sizes).  ``add_rms_norm``, ``linear8`` and ``cross_attention`` take torch tensors on the GPU, check
+them, allocate what they return and run on the current stream of the tensors' device.  There is no fallback: every step
+runs in the library's HIP kernels.
 """
 from __future__ import annotations
 
@@ -20,12 +21,21 @@ _CODES = {torch.float32: M.MAFAT_F32, torch.bfloat16: M.MAFAT_BF16, F8: MAFAT_F8
 _NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, "f8": F8}
 
 # Every symbol include/mafat_reader.h declares.
-EXPORTS = ("mafat_add_rms_norm", "mafat_linear_workspace", "mafat_linear")
+EXPORTS = ("mafat_add_rms_norm", "mafat_linear_workspace", "mafat_linear", "mafat_cross_workspace",
+           "mafat_cross_attention")
 
 
 class mafat_adapters(ctypes.Structure):
     _fields_ = [("count", ctypes.c_int32), ("rank", ctypes.c_int32), ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
                 ("factor", ctypes.c_void_p), ("of_row", ctypes.c_void_p)]
+
+
+class mafat_cross(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("frames", ctypes.c_int32), ("rows", ctypes.c_int64), ("positions", ctypes.c_int64),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+                    "q_row", "q_head", "k_frame", "k_pos", "k_head", "v_frame", "v_pos", "v_head", "y_row", "y_head",
+                    "mask_row")] + [("mask_by_row", ctypes.c_int32)]
 
 
 _ready = None
@@ -41,6 +51,9 @@ def lib():
         adp, sz = ctypes.POINTER(mafat_adapters), ctypes.c_size_t
         L.mafat_linear_workspace.argtypes = [i64, i64, i64, adp, ctypes.POINTER(sz)]
         L.mafat_linear.argtypes = [i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, adp, vp, i64, vp, sz, vp]
+        crp = ctypes.POINTER(mafat_cross)
+        L.mafat_cross_workspace.argtypes = [crp, ctypes.POINTER(sz)]
+        L.mafat_cross_attention.argtypes = [crp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         _ready = L
     return _ready
 
@@ -143,6 +156,20 @@ def mafat_linear(rows, in_cols, out_cols, x, x_stride, x_scale, w, w_stride, w_s
                                 stream))
 
 
+def mafat_cross_workspace(c):
+    """Bytes of workspace of a mafat_cross."""
+    n = ctypes.c_size_t()
+    M._check("mafat_cross_workspace", lib().mafat_cross_workspace(ctypes.byref(c), ctypes.byref(n)))
+    return n.value
+
+
+def mafat_cross_attention(c, q, k, v, q_offsets, k_lengths, mask, y, lse, workspace, ws_bytes, stream):
+    """c: a mafat_cross; device pointers (int or None), stream: hipStream_t (int)."""
+    M._check("mafat_cross_attention",
+             lib().mafat_cross_attention(ctypes.byref(c), q, k, v, q_offsets, k_lengths, mask, y, lse, workspace, ws_bytes,
+                                         stream))
+
+
 # ------------------------------------------------------------------ on tensors
 
 def add_rms_norm(x, gain=None, residual=None, eps=1e-6, out="f8"):
@@ -207,3 +234,52 @@ def linear8(x, x_scale, w, w_scale, bias=None, adapters=None, row_adapter=None):
     _call("mafat_linear", dev, rows, k, n, x.data_ptr(), _row_stride(x, "x"), _ptr(x_scale), w.data_ptr(), w_stride,
           _ptr(w_scale), _ptr(bias), ad, y.data_ptr(), n, _ptr(ws), ws_bytes)
     return y
+
+
+def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_mask=None, scale=None, lse=False):
+    """(y, lse): attention of query rows to the positions of the frames they are about, y in q's type.
+
+    q: [rows, q_heads, d], the rows of all requests about frame 0, then those about frame 1, ...; k, v: [frames, positions,
+    kv_heads, d] (e.g. the halves of a network's output channels; strides are free but for d's), all float32 or all
+    bfloat16; q_heads a multiple of kv_heads, d up to 256.  q_offsets: int32 [frames + 1], frame f's rows are q_offsets[f]
+    to q_offsets[f + 1] (None: rows / frames each; rows that no frame has come back undefined).  k_lengths: int32
+    [frames], the valid positions of each (None: all).  key_mask: bool [frames, positions] or row_mask: bool [rows,
+    positions], true where a position may be read.  scale: of q . k (None: 1 / sqrt(d)).  lse=True: the logarithm of each
+    row's sum of exponentials, float32 [rows, q_heads], -inf for rows without any position (their y is 0); else None.
+    """
+    _need(q.is_cuda and q.dim() == 3 and q.dtype in (torch.float32, torch.bfloat16),
+          "q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
+    rows, hq, d = q.shape
+    dev = q.device
+    _need(k.dim() == 4 and k.shape == v.shape and k.shape[3] == d and k.dtype == q.dtype and v.dtype == q.dtype and
+          k.device == dev and v.device == dev, f"k and v must be {q.dtype} tensors [frames, positions, heads, {d}] on {dev}")
+    frames, positions, hkv, _ = k.shape
+    _need(frames > 0 and hkv > 0 and hq > 0 and d > 0 and hq % hkv == 0,
+          "there must be frames and heads, q's heads a multiple of k's")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        _need(d == 1 or t.stride(-1) == 1, f"{name} must have contiguous values of a head")
+    _vector(q_offsets, frames + 1, torch.int32, dev, "q_offsets")
+    _vector(k_lengths, frames, torch.int32, dev, "k_lengths")
+    _need(key_mask is None or row_mask is None, "key_mask and row_mask exclude each other")
+    mask, by_row, m_row = (key_mask, 0, 0) if row_mask is None else (row_mask, 1, 0)
+    if mask is not None:
+        n = rows if by_row else frames
+        _need(mask.dtype == torch.bool and mask.shape == (n, positions) and mask.device == dev,
+              f"the mask must be a bool tensor of shape {(n, positions)} on {dev}")
+        m_row = _row_stride(mask, "the mask") if positions else 0
+    y = torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
+    got = torch.empty((rows, hq), dtype=torch.float32, device=dev) if lse else None
+
+    def of(t, i):  # an axis of one entry, or of a tensor without entries, may have any stride
+        return t.stride(i) if t.shape[i] > 1 and t.numel() else max(t.stride(i), d)
+
+    c = mafat_cross(_CODES[q.dtype], frames, rows, positions, hq, hkv, d, 1 / math.sqrt(d) if scale is None else scale,
+                    of(q, 0), of(q, 1), of(k, 0), of(k, 1), of(k, 2), of(v, 0), of(v, 1), of(v, 2), hq * d, d, m_row, by_row)
+    ref = ctypes.byref(c)
+    need = ctypes.c_size_t()
+    fn = (_ready or lib()).mafat_cross_workspace
+    M._check("mafat_cross_workspace", fn(ref, ctypes.byref(need)))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _call("mafat_cross_attention", dev, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_offsets), _ptr(k_lengths),
+          _ptr(mask), y.data_ptr(), _ptr(got), _ptr(ws), need.value)
+    return y, got

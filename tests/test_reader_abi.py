@@ -91,3 +91,53 @@ def test_linear_workspace_and_no_rows():
     assert O.lib().mafat_linear_workspace(20, 64, 48, None, None) == EINVAL
     assert O.lib().mafat_linear(*dict(LINEAR, rows=0).values()) == 0
     assert O.lib().mafat_linear(*dict(LINEAR, rows=0, adapters=_adapters(), ws_bytes=0, workspace=None).values()) == 0
+
+
+CROSS = dict(dtype=BF16, frames=2, rows=6, positions=40, q_heads=4, kv_heads=2, head_dim=64, scale=0.125, q_row=256, q_head=64,
+             k_frame=40 * 256, k_pos=256, k_head=64, v_frame=40 * 256, v_pos=256, v_head=64, y_row=256, y_head=64, mask_row=40,
+             mask_by_row=0)
+CALL = dict(q=A, k=B, v=B + 256, q_offsets=C, k_lengths=C + 4096, mask=C + 8192, y=D, lse=D + (1 << 30), workspace=E,
+            ws_bytes=1 << 30, stream=None)
+
+
+def _cross(shape, call):
+    import ctypes
+    return O.lib().mafat_cross_attention(ctypes.byref(O.mafat_cross(**dict(CROSS, **shape))), *dict(CALL, **call).values())
+
+
+@pytest.mark.parametrize("shape, call, status", [
+    (dict(dtype=F8), {}, EUNSUPPORTED), (dict(frames=0), {}, EINVAL), (dict(rows=-1), {}, EINVAL),
+    (dict(positions=-1), {}, EINVAL), (dict(q_heads=3), {}, EINVAL), (dict(kv_heads=0), {}, EINVAL),
+    (dict(q_heads=0), {}, EINVAL), (dict(head_dim=0), {}, EINVAL),
+    (dict(head_dim=257, q_head=257, k_head=257, v_head=257, y_head=257, q_row=1028, y_row=1028, k_pos=514, v_pos=514,
+          k_frame=20560, v_frame=20560), {}, EUNSUPPORTED),
+    (dict(scale=float("inf")), {}, EINVAL), (dict(scale=float("nan")), {}, EINVAL),
+    (dict(q_head=63), {}, EINVAL), (dict(k_head=0), {}, EINVAL), (dict(v_head=-64), {}, EINVAL), (dict(y_head=1), {}, EINVAL),
+    (dict(q_row=10), {}, EINVAL), (dict(y_row=0), {}, EINVAL), (dict(k_pos=0), {}, EINVAL), (dict(v_frame=0), {}, EINVAL),
+    (dict(mask_row=39), {}, EINVAL), (dict(mask_row=-1), {}, EINVAL),
+    (dict(rows=1 << 30), {}, EUNSUPPORTED), (dict(positions=1 << 31), {}, EUNSUPPORTED),
+    (dict(k_pos=1 << 30), {}, EUNSUPPORTED), (dict(q_row=1 << 30), {}, EUNSUPPORTED), (dict(k_frame=1 << 58), {}, EUNSUPPORTED),
+    (dict(kv_heads=65536, q_heads=65536), {}, EUNSUPPORTED),
+    (dict(rows=5), dict(q_offsets=None), EINVAL),
+    ({}, dict(q=None), EINVAL), ({}, dict(k=None), EINVAL), ({}, dict(v=None), EINVAL), ({}, dict(y=None), EINVAL),
+    ({}, dict(q=A + 1), EINVAL), (dict(dtype=F32), dict(k=B + 2), EINVAL), ({}, dict(q_offsets=C + 2), EINVAL),
+    ({}, dict(k_lengths=C + 4097), EINVAL), ({}, dict(lse=D + (1 << 30) + 1), EINVAL),
+    ({}, dict(y=A), EINVAL), ({}, dict(y=B + 2 * 40 * 256 * 2 - 2), EINVAL), ({}, dict(lse=D), EINVAL), ({}, dict(lse=C), EINVAL),
+    (dict(positions=40000, k_frame=40000 * 256, v_frame=40000 * 256, mask_row=40000), dict(ws_bytes=0), M.MAFAT_EWORKSPACE),
+    (dict(positions=40000, k_frame=40000 * 256, v_frame=40000 * 256, mask_row=40000), dict(workspace=None), EINVAL),
+    (dict(positions=40000, k_frame=40000 * 256, v_frame=40000 * 256, mask_row=40000), dict(workspace=E + 16), EINVAL),
+    (dict(positions=40000, k_frame=40000 * 256, v_frame=40000 * 256, mask_row=40000), dict(workspace=D), EINVAL),
+])
+def test_cross_refusals(shape, call, status):
+    rc = _cross(shape, call)
+    assert rc == status, O.lib().mafat_last_error()
+    assert O.lib().mafat_last_error()
+
+
+def test_cross_without_a_shape_or_rows():
+    import ctypes
+    assert O.lib().mafat_cross_attention(None, *CALL.values()) == EINVAL
+    n = ctypes.c_size_t()
+    assert O.lib().mafat_cross_workspace(None, ctypes.byref(n)) == EINVAL
+    assert O.lib().mafat_cross_workspace(ctypes.byref(O.mafat_cross(**CROSS)), None) == EINVAL
+    assert _cross(dict(rows=0), dict(q=None, y=None, workspace=None, ws_bytes=0)) == 0
