@@ -198,6 +198,15 @@ def test_scores_far_apart_and_equal(rows, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 2.0])
+@pytest.mark.parametrize("rows", [2, 200])
+def test_scales(rows, scale, dtype):
+    require_gpu()
+    _check(_make(2, rows, 150, 4, 2, 64, dtype, 7, ragged=True, mask="keys"), scale=scale)
+
+
+@pytest.mark.gpu
 def test_offsets_and_lengths_out_of_range_stay_inside():
     require_gpu()
     import torch
