@@ -92,7 +92,7 @@ int check_cross(const mafat_cross* c, size_t* bytes) {
   if (!fits(c->rows, c->q_row) || !fits(c->rows, c->y_row) || !fits(c->positions, c->k_pos) || !fits(c->positions, c->v_pos) ||
       !fits(c->frames, c->k_frame) || !fits(c->frames, c->v_frame) || !fits(c->mask_by_row ? c->rows : c->frames, c->mask_row))
     return fail(MAFAT_EUNSUPPORTED, "an extent of 2^58 or more");
-  const int splits = cross_splits(*c);
+  const int splits = plan_cross(*c).splits;
   *bytes = splits > 1 ? (static_cast<size_t>(splits) * static_cast<size_t>(c->rows) * c->q_heads * (c->head_dim + 2) * 4 + 255) & ~size_t{255}
                       : 0;
   return MAFAT_OK;
@@ -283,8 +283,9 @@ extern "C" int mafat_cross_attention(const mafat_cross* c, const void* q, const 
     a.frames = c->frames; a.rows = static_cast<int32_t>(c->rows); a.positions = static_cast<int32_t>(c->positions);
     a.q_heads = c->q_heads; a.kv_heads = c->kv_heads; a.group = c->q_heads / c->kv_heads; a.head_dim = c->head_dim;
     a.mask_by_row = c->mask_by_row ? 1 : 0;
-    a.splits = cross_splits(*c);
+    const CrossPlan plan = plan_cross(*c);
+    a.splits = plan.splits;
     a.scale = static_cast<float>(static_cast<double>(c->scale) * 1.4426950408889634);
-    return launched(launch_cross(c->dtype, a, static_cast<hipStream_t>(stream)), "cross attention");
+    return launched(launch_cross(c->dtype, a, plan, static_cast<hipStream_t>(stream)), "cross attention");
   });
 }

@@ -65,8 +65,19 @@ struct CrossArgs {
   int32_t row_blocks;  // blocks of query rows, of all frames together (at most)
   float scale;         // times log2(e): scores are in base 2
 };
-// Splits of the positions that a call's blocks are launched with.
-int cross_splits(const mafat_cross& c);
-hipError_t launch_cross(int dtype, const CrossArgs& a, hipStream_t stream);
+// How a call is cut up, from its sizes alone (the workspace depends on it).
+struct CrossPlan {
+  int splits;  // of the positions, joined afterwards
+  int few;     // 1: the kernel for few rows (bfloat16)
+  int waves;   // of the kernel for many rows (bfloat16): 32 rows each
+};
+constexpr int kMaxCrossSplits = 64;  // one per lane of the joining wave
+CrossPlan plan_cross(const mafat_cross& c);
+// Waves of a block of the kernel for few rows, which share a split's positions.
+constexpr int cross_few_waves(int head_dim) { return head_dim <= 64 ? 4 : 2; }
+// Blocks of `tile` rows of all frames together, at most.
+int64_t cross_row_blocks(const CrossArgs& a, int tile);
+hipError_t launch_cross(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
+hipError_t launch_cross_bf16(const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
 
 }  // namespace mafat
