@@ -65,8 +65,9 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
   const int r = at.tile0 + 32 * (wave & 1) + c;
   const bool real = r < at.tile_rows;
   const int rr = real ? r : at.tile_rows - 1;
-  const int64_t row = at.row0 + rr / a.group;
-  const int head = head0 + rr % a.group;
+  const int in_frame = static_cast<int>(static_cast<uint32_t>(rr) / static_cast<uint32_t>(a.group));
+  const int64_t row = at.row0 + in_frame;
+  const int head = head0 + rr - in_frame * a.group;
 
   // Q^T fragments: piece t of lane half h holds values 2 V t + V h ...
   u32x4 qf[PIECES / 2];
@@ -85,9 +86,9 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
     for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
   float most = kNone, sum = 0.f;
 
-  const int tiles = (at.keys + kKeyTile - 1) / kKeyTile;
-  const int first = static_cast<int>(static_cast<int64_t>(tiles) * split / a.splits);
-  const int last = static_cast<int>(static_cast<int64_t>(tiles) * (split + 1) / a.splits);
+  const int tiles = static_cast<int>((static_cast<uint32_t>(at.keys) + kKeyTile - 1) / kKeyTile);
+  int first, last;
+  part_of(tiles, split, a.splits, &first, &last);
   const T* kb = static_cast<const T*>(a.k) + at.frame * a.k_frame + static_cast<int64_t>(blockIdx.y) * a.k_head;
   const T* vb = static_cast<const T*>(a.v) + at.frame * a.v_frame + static_cast<int64_t>(blockIdx.y) * a.v_head;
   const unsigned char* frame_mask = MASK == MASK_KEYS ? a.mask + at.frame * a.mask_row : nullptr;
@@ -249,8 +250,9 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
 }
 
 // Joins the splits' parts: a block per (query row, head), its four waves taking
-// every fourth split.  Bound by latency: a lane holds one split's weight, so
-// that the parts are all asked for at once.
+// every fourth split.  Bound by latency, so everything is asked for before
+// anything is used: the parts of the first 16 splits, and the statistics, of
+// one split by each lane.
 template <int DT>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
   using T = typename Elt<DT>::T;
@@ -258,19 +260,29 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
   const int lane = static_cast<int>(threadIdx.x) & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int64_t pairs = static_cast<int64_t>(a.rows) * a.q_heads, pair = blockIdx.x;
-  const int64_t row = pair / a.q_heads;
+  const int D = a.head_dim;
+  const float* stat = a.part + static_cast<int64_t>(a.splits) * pairs * D + pair * 2;
+  const float* po = a.part + pair * D + lane;
+  float v[4][4];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        v[j][k] = s0 + 4 * j < a.splits && lane + 64 * k < D ? po[(s0 + 4 * j) * pairs * D + 64 * k] : 0.f;
+  };
+  fetch(wave);
+  float most = kNone, sum = 0.f;
+  if (lane < a.splits) {
+    most = stat[lane * pairs * 2];
+    sum = stat[lane * pairs * 2 + 1];
+  }
+  const int64_t row = static_cast<uint32_t>(pair) / static_cast<uint32_t>(a.q_heads);  // rows * q_heads < 2^31
   const int head = static_cast<int>(pair - row * a.q_heads);
   if (a.q_offsets) {
     // a row that no frame has is not written (its parts were not, either)
     const int lo = min(max(a.q_offsets[0], 0), a.rows), hi = min(max(a.q_offsets[a.frames], 0), a.rows);
     if (row < lo || row >= hi) return;
-  }
-  const int D = a.head_dim;
-  const float* stat = a.part + static_cast<int64_t>(a.splits) * pairs * D + pair * 2;
-  float most = kNone, sum = 0.f;
-  if (lane < a.splits) {
-    most = stat[lane * pairs * 2];
-    sum = stat[lane * pairs * 2 + 1];
   }
   float top = most;
 #pragma unroll
@@ -280,16 +292,14 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   float o[4] = {0.f, 0.f, 0.f, 0.f};
-  const float* po = a.part + pair * D + lane;
   for (int s0 = wave; s0 < a.splits; s0 += 16) {
+    if (s0 != wave) fetch(s0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int s = s0 + 4 * j;
-      if (s >= a.splits) break;
-      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
+      if (s0 + 4 * j >= a.splits) break;
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + 4 * j));
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (lane + 64 * k < D) o[k] = fmaf(po[s * pairs * D + 64 * k], w, o[k]);
+      for (int k = 0; k < 4; ++k) o[k] = fmaf(v[j][k], w, o[k]);
     }
   }
 #pragma unroll

@@ -114,8 +114,9 @@ struct Rows {
     const int r = at.tile0 + tile_row + c, D = a.head_dim;
     real = r < at.tile_rows;
     const int rr = real ? r : at.tile_rows - 1;
-    row = at.row0 + rr / a.group;
-    head = kv * a.group + rr % a.group;
+    const int in_frame = static_cast<int>(static_cast<uint32_t>(rr) / static_cast<uint32_t>(a.group));
+    row = at.row0 + in_frame;
+    head = kv * a.group + rr - in_frame * a.group;
     // A negative scale goes into the rows' sign, so that the largest product has
     // the largest score; a scale of zero makes them zero (minus infinity stands
     // for masked keys and must not meet it).
@@ -125,8 +126,9 @@ struct Rows {
     const uint16_t* q = static_cast<const uint16_t*>(a.q) + row * a.q_row + static_cast<int64_t>(head) * a.q_head;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const int d = 16 * t + 8 * h;
-      qf[t] = load16(q + d, D - d);
+      const int d = 16 * t + 8 * h;  // pieces are whole: head_dim is a multiple of 8
+      qf[t] = u32x4{0, 0, 0, 0};
+      if (d < D) __builtin_memcpy(&qf[t], q + d, 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) qf[t][i] = (qf[t][i] ^ flip) & keep;
     }
@@ -342,13 +344,13 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   // head by head, so that the blocks that share keys and values share an XCD's cache
   const int id = xcd_remap(static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
-  const int kv = id / a.row_blocks;
+  const int kv = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.row_blocks));
   const Place at = find<32 * NW>(a, id - kv * a.row_blocks);
   if (!at.any) return;
   const int split = static_cast<int>(blockIdx.y);
-  const int tiles = static_cast<int>((static_cast<int64_t>(at.keys) + KT - 1) / KT);
-  const int first = static_cast<int>(static_cast<int64_t>(tiles) * split / a.splits);
-  const int last = static_cast<int>(static_cast<int64_t>(tiles) * (split + 1) / a.splits);
+  const int tiles = static_cast<int>((static_cast<uint32_t>(at.keys) + KT - 1) / KT);
+  int first, last;
+  part_of(tiles, split, a.splits, &first, &last);
   Fetch<DP, KT, LOADS, NW> fk, fv;
   fk.template start<false>(a.k, at.frame * a.k_frame + kv * a.k_head, a.k_pos, a.head_dim, at.keys, wave);
   fv.template start<true>(a.v, at.frame * a.v_frame + kv * a.v_head, a.v_pos, a.head_dim, at.keys, wave);
@@ -414,7 +416,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
 template <int DP, int MASK>
 __global__ __launch_bounds__(64 * cross_few_waves(DP), 1) void cross_few_kernel(const CrossArgs a) {
   using F = Fast<DP>;
-  constexpr int NW = cross_few_waves(DP), SLOTS = DP <= 128 ? 4 : 2;
+  constexpr int NW = cross_few_waves(DP), SLOTS = DP <= 64 ? 4 : 2;
   constexpr int KT = 32, HALF = KT * F::PITCH, LOADS = KT / F::ROWS;
   constexpr int NT = DP / 32, JOIN = 32 * DP + 64;  // floats of a wave's part: sums, statistics of 32 rows
   static_assert((SLOTS - 1) * 2 * LOADS <= 63, "loads in flight that a wave can count");
@@ -423,13 +425,13 @@ __global__ __launch_bounds__(64 * cross_few_waves(DP), 1) void cross_few_kernel(
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int id = xcd_remap(static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
-  const int kv = id / a.row_blocks;
+  const int kv = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.row_blocks));
   const Place at = find<32>(a, id - kv * a.row_blocks);
   if (!at.any) return;
   const int split = static_cast<int>(blockIdx.y);
-  const int64_t tiles = (static_cast<int64_t>(at.keys) + KT - 1) / KT;
-  const int64_t part = static_cast<int64_t>(split) * NW + wave, parts = static_cast<int64_t>(a.splits) * NW;
-  const int first = static_cast<int>(tiles * part / parts), last = static_cast<int>(tiles * (part + 1) / parts);
+  const int tiles = static_cast<int>((static_cast<uint32_t>(at.keys) + KT - 1) / KT);
+  int first, last;
+  part_of(tiles, split * NW + wave, a.splits * NW, &first, &last);
   Fetch<DP, KT, LOADS, 1> fk, fv;
   fk.template start<false>(a.k, at.frame * a.k_frame + kv * a.k_head, a.k_pos, a.head_dim, at.keys, 0);
   fv.template start<true>(a.v, at.frame * a.v_frame + kv * a.v_head, a.v_pos, a.head_dim, at.keys, 0);

@@ -37,6 +37,15 @@ __device__ __forceinline__ u32x4 load16(const T* p, int n) {
 // Key of a 32-key tile that accumulator register i of a lane of half h holds.
 __device__ __forceinline__ int key_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
+// The i-th of n parts of `all` tiles, as even as they go: [first, last).  (One
+// 32-bit division: these run ahead of a block's first load.)
+__device__ __forceinline__ void part_of(int all, int i, int n, int* first, int* last) {
+  const uint32_t per = static_cast<uint32_t>(all) / static_cast<uint32_t>(n);
+  const int more = all - static_cast<int>(per) * n;  // the first `more` parts have one more
+  *first = static_cast<int>(per) * i + min(i, more);
+  *last = *first + static_cast<int>(per) + (i < more ? 1 : 0);
+}
+
 // A block's work: a row tile of a frame.
 struct Place {
   int frame, row0, tile0, tile_rows, keys;  // first query row, first pair of the tile, pairs of the frame, valid positions
@@ -49,21 +58,24 @@ template <int RT>
 __device__ __forceinline__ Place find(const CrossArgs& a, int b) {
   Place p;
   p.any = true;
+  p.keys = a.positions;
   if (!a.q_offsets) {
-    const int per = a.rows / a.frames, blocks = static_cast<int>((static_cast<int64_t>(per) * a.group + RT - 1) / RT);
-    p.frame = b / blocks;
+    const int per = a.per_frame, blocks = static_cast<int>((static_cast<uint32_t>(per * a.group) + RT - 1) / RT);
+    p.frame = static_cast<int>(static_cast<uint32_t>(b) / static_cast<uint32_t>(blocks));
     p.row0 = p.frame * per;
     p.tile0 = (b - p.frame * blocks) * RT;
     p.tile_rows = per * a.group;
     p.any = p.frame < a.frames;
+    if (p.any && a.k_lengths) p.keys = min(max(a.k_lengths[p.frame], 0), a.positions);
   } else {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     int before = 0;
     p.any = false;
     for (int f0 = 0; f0 < a.frames; f0 += 64) {
       const int f = f0 + lane;
-      int lo = 0, n = 0;
+      int lo = 0, n = 0, keys = a.positions;
       if (f < a.frames) {
+        if (a.k_lengths) keys = min(max(a.k_lengths[f], 0), a.positions);
         lo = min(max(a.q_offsets[f], 0), a.rows);
         n = max(min(max(a.q_offsets[f + 1], 0), a.rows) - lo, 0);
       }
@@ -83,6 +95,7 @@ __device__ __forceinline__ Place find(const CrossArgs& a, int b) {
         const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
         p.frame = f0 + l;
         p.row0 = __builtin_amdgcn_readlane(lo, l);
+        p.keys = __builtin_amdgcn_readlane(keys, l);
         p.tile_rows = __builtin_amdgcn_readlane(pairs, l);
         p.tile0 = (b - __builtin_amdgcn_readlane(from, l)) * RT;
         p.any = true;
@@ -91,8 +104,6 @@ __device__ __forceinline__ Place find(const CrossArgs& a, int b) {
       before = static_cast<int>(static_cast<uint32_t>(before) + static_cast<uint32_t>(__builtin_amdgcn_readlane(upto, 63)));
     }
   }
-  p.keys = 0;
-  if (p.any) p.keys = a.k_lengths ? min(max(a.k_lengths[p.frame], 0), a.positions) : a.positions;
   return p;
 }
 

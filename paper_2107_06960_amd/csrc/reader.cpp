@@ -283,6 +283,7 @@ extern "C" int mafat_cross_attention(const mafat_cross* c, const void* q, const 
     a.frames = c->frames; a.rows = static_cast<int32_t>(c->rows); a.positions = static_cast<int32_t>(c->positions);
     a.q_heads = c->q_heads; a.kv_heads = c->kv_heads; a.group = c->q_heads / c->kv_heads; a.head_dim = c->head_dim;
     a.mask_by_row = c->mask_by_row ? 1 : 0;
+    a.per_frame = static_cast<int32_t>(c->rows / c->frames);
     const CrossPlan plan = plan_cross(*c);
     a.splits = plan.splits;
     a.scale = static_cast<float>(static_cast<double>(c->scale) * 1.4426950408889634);

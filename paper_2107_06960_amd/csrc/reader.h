@@ -62,6 +62,7 @@ struct CrossArgs {
   int32_t frames, rows, positions, q_heads, kv_heads, group, head_dim;
   int32_t mask_by_row;
   int32_t splits;
+  int32_t per_frame;   // query rows of a frame, without offsets
   int32_t row_blocks;  // blocks of query rows, of all frames together (at most)
   float scale;         // times log2(e): scores are in base 2
 };
@@ -74,7 +75,7 @@ struct CrossPlan {
 constexpr int kMaxCrossSplits = 64;  // one per lane of the joining wave
 CrossPlan plan_cross(const mafat_cross& c);
 // Waves of a block of the kernel for few rows, which share a split's positions.
-constexpr int cross_few_waves(int head_dim) { return head_dim <= 64 ? 4 : 2; }
+constexpr int cross_few_waves(int head_dim) { return head_dim <= 128 ? 4 : 2; }
 // Blocks of `tile` rows of all frames together, at most.
 int64_t cross_row_blocks(const CrossArgs& a, int tile);
 hipError_t launch_cross(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t stream);

@@ -9,6 +9,7 @@ runs in the library's HIP kernels.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 
 import torch
@@ -58,38 +59,26 @@ def lib():
     return _ready
 
 
-def _raw_stream(device):
-    """The current stream of `device`, as M._stream_handle gives it for the current one."""
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is not None:
-        return raw(device.index)
-    return torch.cuda.current_stream(device).cuda_stream
+# The host's time counts where a call takes a few microseconds on the GPU: the
+# current device and stream are asked for without building objects where torch
+# offers that, and texts are put together only for an error.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-class _On:
-    """Makes `device` the current one for a call, if it is not."""
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
-
-
-def _call(name, device, *args):
-    """One C call on the current stream of `device`, its last argument."""
+def _call(name, index, *args):
+    """One C call on the current stream of device `index`, the call's last argument."""
     fn = getattr(_ready or lib(), name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, _raw_stream(device))
+    before = _current_device()
+    if before == index:
+        rc = fn(*args, _raw_stream(index))
     else:
-        with _On(device):
-            rc = fn(*args, _raw_stream(device))
+        torch.cuda.set_device(index)
+        try:
+            rc = fn(*args, _raw_stream(index))
+        finally:
+            torch.cuda.set_device(before)
     if rc:
         M._check(name, rc)
 
@@ -98,34 +87,35 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _need(ok, text):
-    if not ok:
-        raise ValueError(text)
+def _refuse(text):
+    raise ValueError(text)
 
 
-def _vector(t, n, dtype, device, name):
-    """An optional contiguous vector of n values."""
-    if t is not None:
-        _need(t.dtype == dtype and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device,
-              f"{name} must be a contiguous {dtype} vector of {n} values on {device}")
-
-
-def _matrix(t, shape, dtype, device, name):
-    """A matrix of contiguous rows; its row stride."""
-    _need(t.dtype == dtype and t.shape == shape and t.device == device,
-          f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return _row_stride(t, name)
+def _vector(t, n, dtype, dev, name):
+    """The address of an optional contiguous vector of n values."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != (n,) or t.device != dev or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} vector of {n} values on {dev}")
+    return t.data_ptr()
 
 
 def _row_stride(t, name):
     """Elements between the rows of a matrix whose rows are contiguous and apart (a single one counts as such)."""
     rows, cols = t.shape
+    s, c = t.stride()
     if rows <= 1:
         s = cols
-    else:
-        s = t.stride(0)
-    _need((cols == 1 or t.stride(1) == 1) and s >= cols, f"{name} must have contiguous rows that do not overlap")
+    if (c != 1 and cols != 1) or s < cols:
+        _refuse(f"{name} must have contiguous rows that do not overlap")
     return s
+
+
+def _matrix(t, shape, dtype, dev, name):
+    """The row stride of a matrix."""
+    if t.dtype is not dtype or t.shape != shape or t.device != dev:
+        _refuse(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return _row_stride(t, name)
 
 
 # ------------------------------------------------------------------ C names
@@ -178,22 +168,30 @@ def add_rms_norm(x, gain=None, residual=None, eps=1e-6, out="f8"):
     x, residual: [rows, cols], float32 or bfloat16, contiguous rows of any stride.  gain: float32 [cols] or None (ones).
     out: "f8" (e4m3 values with a float32 scale per row: y times scale is the norm), "bf16" or "f32" (scale is None).
     """
-    _need(x.is_cuda and x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16),
-          "x must be a float32 or bfloat16 matrix on the GPU")
+    dt, to = x.dtype, _NAMES.get(out)
+    if not x.is_cuda or x.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        _refuse("x must be a float32 or bfloat16 matrix on the GPU")
+    if to is None:
+        _refuse(f"out must be one of {sorted(_NAMES)}, not {out!r}")
     rows, cols = x.shape
-    _need(cols > 0, "x has no columns")
-    dev, to = x.device, _NAMES.get(out)
-    _need(to is not None, f"out must be one of {sorted(_NAMES)}, not {out!r}")
-    _vector(gain, cols, torch.float32, dev, "gain")
-    h = None
+    if cols < 1:
+        _refuse("x has no columns")
+    dev = x.device
+    x_stride = _row_stride(x, "x")
+    gain_at = _vector(gain, cols, torch.float32, dev, "gain")
+    h = h_at = res_at = None
     r_stride = cols
     if residual is not None:
-        r_stride = _matrix(residual, x.shape, x.dtype, dev, "residual")
-        h = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+        r_stride = _matrix(residual, x.shape, dt, dev, "residual")
+        h = torch.empty((rows, cols), dtype=dt, device=dev)
+        h_at, res_at = h.data_ptr(), residual.data_ptr()
     y = torch.empty((rows, cols), dtype=to, device=dev)
-    scale = torch.empty(rows, dtype=torch.float32, device=dev) if to is F8 else None
-    _call("mafat_add_rms_norm", dev, rows, cols, _CODES[x.dtype], x.data_ptr(), _row_stride(x, "x"), _ptr(residual),
-          r_stride, _ptr(gain), eps, _ptr(h), cols, _CODES[to], y.data_ptr(), cols, _ptr(scale))
+    scale = scale_at = None
+    if to is F8:
+        scale = torch.empty(rows, dtype=torch.float32, device=dev)
+        scale_at = scale.data_ptr()
+    _call("mafat_add_rms_norm", dev.index, rows, cols, _CODES[dt], x.data_ptr(), x_stride, res_at, r_stride, gain_at, eps,
+          h_at, cols, _CODES[to], y.data_ptr(), cols, scale_at)
     return h, y, scale
 
 
@@ -205,34 +203,38 @@ def linear8(x, x_scale, w, w_scale, bias=None, adapters=None, row_adapter=None):
     bfloat16 [count, out, rank], factor float32 [count] or None, with row_adapter int32 [rows]: row i gets
     factor[j] * (x_i a[j]^T) b[j]^T for j = row_adapter[i], nothing where that is outside [0, count).
     """
-    _need(x.is_cuda and x.dim() == 2 and w.dim() == 2 and x.dtype is F8, "x and w must be float8_e4m3fn matrices on the GPU")
+    if not x.is_cuda or x.dim() != 2 or w.dim() != 2 or x.dtype is not F8:
+        _refuse("x and w must be float8_e4m3fn matrices on the GPU")
     rows, k = x.shape
     n, dev = w.shape[0], x.device
-    _need(k > 0 and n > 0, "x and w must have columns and rows")
-    w_stride = _matrix(w, (n, k), F8, dev, "w")
-    _vector(x_scale, rows, torch.float32, dev, "x_scale")
-    _vector(w_scale, n, torch.float32, dev, "w_scale")
-    _vector(bias, n, torch.float32, dev, "bias")
-    _need((adapters is None) == (row_adapter is None), "adapters and row_adapter go together")
+    if k < 1 or n < 1:
+        _refuse("x and w must have columns and rows")
+    x_stride, w_stride = _row_stride(x, "x"), _matrix(w, (n, k), F8, dev, "w")
+    x_scale_at = _vector(x_scale, rows, torch.float32, dev, "x_scale")
+    w_scale_at = _vector(w_scale, n, torch.float32, dev, "w_scale")
+    bias_at = _vector(bias, n, torch.float32, dev, "bias")
+    if (adapters is None) != (row_adapter is None):
+        _refuse("adapters and row_adapter go together")
     y = torch.empty((rows, n), dtype=torch.bfloat16, device=dev)
     ad = ws = None
     ws_bytes = 0
     if adapters is not None:
         a, b, factor = adapters
-        count, rank = a.shape[0], a.shape[1]
-        _need(count > 0 and rank > 0, "adapters must not be empty")
-        for t, shape, name in ((a, (count, rank, k), "adapters' a"), (b, (count, n, rank), "adapters' b")):
-            _need(t.dtype == torch.bfloat16 and t.shape == shape and t.is_contiguous() and t.device == dev,
-                  f"{name} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
-        _vector(factor, count, torch.float32, dev, "adapters' factor")
-        _vector(row_adapter, rows, torch.int32, dev, "row_adapter")
-        ad = ctypes.byref(mafat_adapters(count, rank, a.data_ptr(), b.data_ptr(), _ptr(factor), row_adapter.data_ptr()))
+        if a.dim() != 3 or a.shape[0] < 1 or a.shape[1] < 1:
+            _refuse("adapters must not be empty")
+        count, rank, _ = a.shape
+        for t, shape, name in ((a, (count, rank, k), "a"), (b, (count, n, rank), "b")):
+            if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != dev or not t.is_contiguous():
+                _refuse(f"adapters' {name} must be a contiguous bfloat16 tensor of shape {shape} on {dev}")
+        factor_at = _vector(factor, count, torch.float32, dev, "adapters' factor")
+        of_row = _vector(row_adapter, rows, torch.int32, dev, "row_adapter")
+        ad = ctypes.byref(mafat_adapters(count, rank, a.data_ptr(), b.data_ptr(), factor_at, of_row))
         need = ctypes.c_size_t()
-        M._check("mafat_linear_workspace", lib().mafat_linear_workspace(rows, k, n, ad, ctypes.byref(need)))
+        M._check("mafat_linear_workspace", (_ready or lib()).mafat_linear_workspace(rows, k, n, ad, ctypes.byref(need)))
         ws_bytes = need.value
         ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-    _call("mafat_linear", dev, rows, k, n, x.data_ptr(), _row_stride(x, "x"), _ptr(x_scale), w.data_ptr(), w_stride,
-          _ptr(w_scale), _ptr(bias), ad, y.data_ptr(), n, _ptr(ws), ws_bytes)
+    _call("mafat_linear", dev.index, rows, k, n, x.data_ptr(), x_stride, x_scale_at, w.data_ptr(), w_stride, w_scale_at,
+          bias_at, ad, y.data_ptr(), n, _ptr(ws), ws_bytes)
     return y
 
 
@@ -247,39 +249,48 @@ def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_
     positions], true where a position may be read.  scale: of q . k (None: 1 / sqrt(d)).  lse=True: the logarithm of each
     row's sum of exponentials, float32 [rows, q_heads], -inf for rows without any position (their y is 0); else None.
     """
-    _need(q.is_cuda and q.dim() == 3 and q.dtype in (torch.float32, torch.bfloat16),
-          "q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
+    dt = q.dtype
+    if not q.is_cuda or q.dim() != 3 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
     rows, hq, d = q.shape
-    dev = q.device
-    _need(k.dim() == 4 and k.shape == v.shape and k.shape[3] == d and k.dtype == q.dtype and v.dtype == q.dtype and
-          k.device == dev and v.device == dev, f"k and v must be {q.dtype} tensors [frames, positions, heads, {d}] on {dev}")
-    frames, positions, hkv, _ = k.shape
-    _need(frames > 0 and hkv > 0 and hq > 0 and d > 0 and hq % hkv == 0,
-          "there must be frames and heads, q's heads a multiple of k's")
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _need(d == 1 or t.stride(-1) == 1, f"{name} must have contiguous values of a head")
-    _vector(q_offsets, frames + 1, torch.int32, dev, "q_offsets")
-    _vector(k_lengths, frames, torch.int32, dev, "k_lengths")
-    _need(key_mask is None or row_mask is None, "key_mask and row_mask exclude each other")
-    mask, by_row, m_row = (key_mask, 0, 0) if row_mask is None else (row_mask, 1, 0)
+    dev, shape = q.device, k.shape
+    if k.dim() != 4 or shape != v.shape or shape[3] != d or k.dtype is not dt or v.dtype is not dt or k.device != dev or \
+            v.device != dev:
+        _refuse(f"k and v must be {dt} tensors [frames, positions, heads, {d}] on {dev}")
+    frames, positions, hkv, _ = shape
+    mask, by_row = (key_mask, 0) if row_mask is None else (row_mask, 1)
+    m_row = 0
     if mask is not None:
-        n = rows if by_row else frames
-        _need(mask.dtype == torch.bool and mask.shape == (n, positions) and mask.device == dev,
-              f"the mask must be a bool tensor of shape {(n, positions)} on {dev}")
+        if key_mask is not None and row_mask is not None:
+            _refuse("key_mask and row_mask exclude each other")
+        if mask.dtype is not torch.bool or mask.shape != (rows if by_row else frames, positions) or mask.device != dev:
+            _refuse(f"the mask must be a bool tensor of shape {(rows if by_row else frames, positions)} on {dev}")
         m_row = _row_stride(mask, "the mask") if positions else 0
-    y = torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
+    offsets_at = _vector(q_offsets, frames + 1, torch.int32, dev, "q_offsets")
+    lengths_at = _vector(k_lengths, frames, torch.int32, dev, "k_lengths")
+    ref, need, _ = _cross_shape(dt, rows, hq, d, frames, positions, hkv, q.stride(), k.stride(), v.stride(), scale, m_row, by_row)
+    y = torch.empty((rows, hq, d), dtype=dt, device=dev)
     got = torch.empty((rows, hq), dtype=torch.float32, device=dev) if lse else None
-
-    def of(t, i):  # an axis of one entry, or of a tensor without entries, may have any stride
-        return t.stride(i) if t.shape[i] > 1 and t.numel() else max(t.stride(i), d)
-
-    c = mafat_cross(_CODES[q.dtype], frames, rows, positions, hq, hkv, d, 1 / math.sqrt(d) if scale is None else scale,
-                    of(q, 0), of(q, 1), of(k, 0), of(k, 1), of(k, 2), of(v, 0), of(v, 1), of(v, 2), hq * d, d, m_row, by_row)
-    ref = ctypes.byref(c)
-    need = ctypes.c_size_t()
-    fn = (_ready or lib()).mafat_cross_workspace
-    M._check("mafat_cross_workspace", fn(ref, ctypes.byref(need)))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-    _call("mafat_cross_attention", dev, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_offsets), _ptr(k_lengths),
-          _ptr(mask), y.data_ptr(), _ptr(got), _ptr(ws), need.value)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call("mafat_cross_attention", dev.index, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets_at, lengths_at, _ptr(mask),
+          y.data_ptr(), _ptr(got), _ptr(ws), need)
     return y, got
+
+
+@functools.lru_cache(maxsize=256)
+def _cross_shape(dt, rows, hq, d, frames, positions, hkv, qs, ks, vs, scale, m_row, by_row):
+    """(reference to the call's mafat_cross, bytes of workspace, the struct itself) for sizes and strides."""
+    if not (frames > 0 and hkv > 0 and hq > 0 and d > 0 and hq % hkv == 0):
+        _refuse("there must be frames and heads, q's heads a multiple of k's")
+    if d > 1 and not qs[2] == ks[3] == vs[3] == 1:
+        _refuse("q, k and v must have contiguous values of a head")
+
+    def of(stride, n, entries):  # an axis of one entry, or of a tensor without entries, may have any stride
+        return stride if n > 1 and entries else max(stride, d)
+
+    some = frames * positions
+    c = mafat_cross(_CODES[dt], frames, rows, positions, hq, hkv, d, 1 / math.sqrt(d) if scale is None else scale,
+                    of(qs[0], rows, rows), of(qs[1], hq, rows), *(of(st[i], n, some) for st in (ks, vs) for i, n in (
+                        (0, frames), (1, positions), (2, hkv))), hq * d, d, m_row, by_row)
+    need = mafat_cross_workspace(c)
+    return ctypes.byref(c), need, c
