@@ -51,6 +51,7 @@ int launched(hipError_t e, const char* what) {
 
 constexpr int64_t kMaxLinearCols = int64_t{1} << 22;  // 256 rows of a tile in 32-bit offsets
 constexpr int kMaxRank = 128;
+constexpr int rank_padded(int rank) { return (rank + 15) & ~15; }  // whole matrix instructions
 
 // The sizes and adapters of a projection; the workspace holds the adapters'
 // inner products of every row.
@@ -62,7 +63,7 @@ int check_linear(int64_t rows, int64_t in_cols, int64_t out_cols, const mafat_ad
   if (ad) {
     if (ad->count < 1 || ad->rank < 1) return fail(MAFAT_EINVAL, "adapters: count and rank must be >= 1");
     if (ad->rank > kMaxRank) return fail(MAFAT_EUNSUPPORTED, "adapters: rank above 128");
-    *bytes = (static_cast<size_t>(rows) * ad->rank * sizeof(float) + 255) & ~size_t{255};
+    *bytes = (static_cast<size_t>(rows) * 2 * rank_padded(ad->rank) * sizeof(uint16_t) + 255) & ~size_t{255};
   }
   return MAFAT_OK;
 }
@@ -206,7 +207,8 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
       a.b = static_cast<const uint16_t*>(d.b);
       a.factor = d.factor;
       a.of_row = d.of_row;
-      a.u = static_cast<float*>(workspace);
+      a.u = static_cast<uint16_t*>(workspace);
+      a.rank_pad = rank_padded(d.rank);
       a.count = d.count;
       a.rank = d.rank;
     } else {

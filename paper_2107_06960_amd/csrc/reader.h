@@ -33,16 +33,17 @@ struct LinearArgs {
   const float* w_scale;
   const float* bias;
   void* y;
-  // adapters (count 0: none); u: float32 [rows][rank], factor * x_scale * (a x)
+  // adapters (count 0: none); u = factor * x_scale * (a x) of every row as two
+  // bfloat16 parts, [rows][2][rank_pad] with zeros past the rank
   const uint16_t* a;
   const uint16_t* b;
   const float* factor;
   const int32_t* of_row;
-  float* u;
+  uint16_t* u;
   int64_t x_stride, w_stride, y_stride;
   int64_t rows;
   int32_t in_cols, out_cols;
-  int32_t count, rank;
+  int32_t count, rank, rank_pad;
 };
 hipError_t launch_linear(const LinearArgs& a, hipStream_t stream);
 
