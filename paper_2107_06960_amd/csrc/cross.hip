@@ -249,18 +249,21 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
     a.lse[row * a.q_heads + head] = sum == 0.f ? kNone : (most + __log2f(sum)) * 0.6931471805599453f;
 }
 
-// Joins the splits' parts: a block per (query row, head), its four waves taking
-// every fourth split.  Bound by latency, so everything is asked for before
-// anything is used: the parts of the first 16 splits, and the statistics, of
-// one split by each lane.
-template <int DT>
+// Joins the splits' parts of a (query row, head) with W waves, each taking every
+// W-th split: all four of a block where there are many splits, one where there
+// are few (and then rather many pairs).  Bound by latency, so everything is
+// asked for before anything is used: the parts of a wave's first four splits,
+// and the statistics, of one split by each lane.
+template <int DT, int W>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
   using T = typename Elt<DT>::T;
-  __shared__ float part[4][256];
+  __shared__ float part[W > 1 ? W : 1][W > 1 ? 256 : 1];
   const int lane = static_cast<int>(threadIdx.x) & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int64_t pairs = static_cast<int64_t>(a.rows) * a.q_heads, pair = blockIdx.x;
-  const int D = a.head_dim;
+  const int64_t pairs = static_cast<int64_t>(a.rows) * a.q_heads;
+  const int64_t pair = W > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
+  if (pair >= pairs) return;
+  const int first = W > 1 ? wave : 0, D = a.head_dim;
   const float* stat = a.part + static_cast<int64_t>(a.splits) * pairs * D + pair * 2;
   const float* po = a.part + pair * D + lane;
   float v[4][4];
@@ -269,9 +272,9 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        v[j][k] = s0 + 4 * j < a.splits && lane + 64 * k < D ? po[(s0 + 4 * j) * pairs * D + 64 * k] : 0.f;
+        v[j][k] = s0 + W * j < a.splits && lane + 64 * k < D ? po[(s0 + W * j) * pairs * D + 64 * k] : 0.f;
   };
-  fetch(wave);
+  fetch(first);
   float most = kNone, sum = 0.f;
   if (lane < a.splits) {
     most = stat[lane * pairs * 2];
@@ -292,25 +295,31 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   float o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = wave; s0 < a.splits; s0 += 16) {
-    if (s0 != wave) fetch(s0);
+  for (int s0 = first; s0 < a.splits; s0 += 4 * W) {
+    if (s0 != first) fetch(s0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (s0 + 4 * j >= a.splits) break;
-      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + 4 * j));
+      if (s0 + W * j >= a.splits) break;
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + W * j));
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] = fmaf(v[j][k], w, o[k]);
     }
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = o[k];
-  __syncthreads();
-  const int d = static_cast<int>(threadIdx.x);
   const float over = sum == 0.f ? 0.f : 1.f / sum;  // no key: zeros
-  if (d < D)
-    store1(static_cast<T*>(a.y) + row * a.y_row + static_cast<int64_t>(head) * a.y_head + d,
-           ((part[0][d] + part[1][d]) + (part[2][d] + part[3][d])) * over);
-  if (a.lse && d == 0) a.lse[pair] = sum == 0.f ? kNone : (top + __log2f(sum)) * 0.6931471805599453f;
+  T* y = static_cast<T*>(a.y) + row * a.y_row + static_cast<int64_t>(head) * a.y_head;
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = o[k];
+    __syncthreads();
+    const int d = static_cast<int>(threadIdx.x);
+    if (d < D) store1(y + d, ((part[0][d] + part[1][d]) + (part[2][d] + part[3][d])) * over);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (lane + 64 * k < D) store1(y + lane + 64 * k, o[k] * over);
+  }
+  if (a.lse && lane == 0 && first == 0)
+    a.lse[pair] = sum == 0.f ? kNone : (top + __log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int DT, int DP>
@@ -339,13 +348,15 @@ hipError_t launch(const CrossArgs& a, const CrossPlan& p, hipStream_t stream) {
     if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits));
     if (a.head_dim <= 64) launch_any<DT, 64>(a, grid, stream);
+    else if (a.head_dim <= 96) launch_any<DT, 96>(a, grid, stream);
     else if (a.head_dim <= 128) launch_any<DT, 128>(a, grid, stream);
     else launch_any<DT, 256>(a, grid, stream);
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL((cross_join_kernel<DT>), dim3(static_cast<unsigned>(a.rows) * static_cast<unsigned>(a.q_heads)), dim3(256), 0,
-                     stream, a);
+  const unsigned pairs = static_cast<unsigned>(a.rows) * static_cast<unsigned>(a.q_heads);
+  if (a.splits > 8) hipLaunchKernelGGL((cross_join_kernel<DT, 4>), dim3(pairs), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((cross_join_kernel<DT, 1>), dim3((pairs + 3) / 4), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -368,7 +379,9 @@ CrossPlan plan_cross(const mafat_cross& c) {
   int64_t want, least;  // blocks that fill the GPU; positions that a split is worth
   if (c.dtype == MAFAT_BF16 && pairs <= 64) {
     p.few = 1;
+    // A block a CU; two where each still streams 512 positions.
     want = 256 / blocks(32);
+    if (want > 0 && c.positions / want >= 1024) want *= 2;
     least = 64 * cross_few_waves(c.head_dim);
   } else if (c.dtype == MAFAT_BF16) {
     if (blocks(256) >= 256) p.waves = 8;
@@ -376,7 +389,7 @@ CrossPlan plan_cross(const mafat_cross& c) {
     least = 256;
   } else {
     want = 512 / blocks(kRowTile);
-    least = 2 * kKeyTile;
+    least = kKeyTile;
   }
   int64_t n = (c.positions + least - 1) / least;
   if (n > want) n = want;

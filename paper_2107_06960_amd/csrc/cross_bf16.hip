@@ -38,9 +38,14 @@ struct Fast {
 // would be waited for at once.  The load has no register result; the kernel
 // waits for it itself (wait_vmcnt) before the barrier that hands the tile on.
 __device__ __forceinline__ void load_to_lds(const u32x4& range, unsigned off, unsigned to) {
+  // (the same in all lanes, which the compiler has to know)
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(range[i])));
+  to = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(to), "v"(off), "s"(range)
+               : "s"(to), "v"(off), "s"(r)
                : "memory");
 }
 // A descriptor of `bytes` bytes from p, as four words.
@@ -412,16 +417,20 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
 
 // Few rows: 32 rows for all waves of a block, each wave streaming 32 keys at a
 // time of a part of its own through SLOTS slots of its own: no wave waits for
-// another before the end, where the parts are joined in LDS.
+// another before the end, where the parts are joined in LDS.  The slots of a
+// block take at most 67 KB, so that two blocks share a CU: their waves fetch
+// while others compute, and a ragged call's blocks run in one round (8 frames,
+// 64 rows, 8 heads of 128, up to 1444 positions: 13.8 us; with twice the slots
+// and one block a CU 17.8).
 template <int DP, int MASK>
 __global__ __launch_bounds__(64 * cross_few_waves(DP), 1) void cross_few_kernel(const CrossArgs a) {
   using F = Fast<DP>;
-  constexpr int NW = cross_few_waves(DP), SLOTS = DP <= 64 ? 4 : 2;
+  constexpr int NW = cross_few_waves(DP), SLOTS = DP <= 64 ? 2 : 1;
   constexpr int KT = 32, HALF = KT * F::PITCH, LOADS = KT / F::ROWS;
   constexpr int NT = DP / 32, JOIN = 32 * DP + 64;  // floats of a wave's part: sums, statistics of 32 rows
   static_assert((SLOTS - 1) * 2 * LOADS <= 63, "loads in flight that a wave can count");
-  static_assert(NW * JOIN * 4 <= NW * SLOTS * 2 * HALF, "the parts fit");
-  __shared__ __align__(1024) unsigned char smem[NW * SLOTS * 2 * HALF];
+  constexpr int RING = NW * SLOTS * 2 * HALF, LDS = RING > NW * JOIN * 4 ? RING : NW * JOIN * 4;
+  __shared__ __align__(1024) unsigned char smem[LDS];
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int id = xcd_remap(static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
