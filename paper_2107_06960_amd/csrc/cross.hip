@@ -329,20 +329,23 @@ void launch_any(const CrossArgs& a, dim3 grid, hipStream_t stream) {
   else hipLaunchKernelGGL((cross_any_kernel<DT, DP, MASK_ROWS>), grid, dim3(256), 0, stream, a);
 }
 
-// Whole 16-byte pieces, and offsets of a tile's 64 rows in 31 bits.
+// Whole 16-byte pieces, offsets of a tile's 64 rows in 31 bits, and heads whose
+// sums fit the registers.
+template <int DT>
 bool fast(const CrossArgs& a) {
+  constexpr int64_t esz = sizeof(typename Elt<DT>::T);
   const auto whole = [](const void* p, int64_t x, int64_t y, int64_t z) {
-    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (x | y | z))) & 15) == 0;
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(esz * (x | y | z))) & 15) == 0;
   };
-  return a.head_dim % 8 == 0 && a.k_pos < (1 << 23) && a.v_pos < (1 << 23) && whole(a.k, a.k_frame, a.k_pos, a.k_head) &&
-         whole(a.v, a.v_frame, a.v_pos, a.v_head);
+  return a.head_dim * esz % 16 == 0 && (DT == MAFAT_BF16 || a.head_dim <= 128) && a.k_pos < (1 << 22) && a.v_pos < (1 << 22) &&
+         whole(a.k, a.k_frame, a.k_pos, a.k_head) && whole(a.v, a.v_frame, a.v_pos, a.v_head);
 }
 
 template <int DT>
 hipError_t launch(const CrossArgs& a, const CrossPlan& p, hipStream_t stream) {
   hipError_t e;
-  if (DT == MAFAT_BF16 && fast(a) && cross_row_blocks(a, 32) * a.kv_heads < (int64_t{1} << 31)) {
-    e = launch_cross_bf16(a, p, stream);
+  if (fast<DT>(a) && cross_row_blocks(a, 32) * a.kv_heads < (int64_t{1} << 31)) {
+    e = DT == MAFAT_BF16 ? launch_cross_bf16(a, p, stream) : launch_cross_f32(a, p, stream);
   } else {
     const int64_t blocks = cross_row_blocks(a, kRowTile);
     if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
@@ -377,19 +380,16 @@ CrossPlan plan_cross(const mafat_cross& c) {
   const int64_t each = static_cast<int64_t>(c.frames) * c.kv_heads;
   const auto blocks = [&](int64_t tile) { return each * ((pairs + tile - 1) / tile); };
   int64_t want, least;  // blocks that fill the GPU; positions that a split is worth
-  if (c.dtype == MAFAT_BF16 && pairs <= 64) {
+  if (pairs <= 64) {
     p.few = 1;
     // A block a CU; two where each still streams 512 positions.
     want = 256 / blocks(32);
     if (want > 0 && c.positions / want >= 1024) want *= 2;
-    least = 64 * cross_few_waves(c.head_dim);
-  } else if (c.dtype == MAFAT_BF16) {
+    least = 64 * cross_few_waves(c.dtype, c.head_dim);
+  } else {
     if (blocks(256) >= 256) p.waves = 8;
     want = (p.waves == 8 ? 256 : 512) / blocks(32 * p.waves);
-    least = 256;
-  } else {
-    want = 512 / blocks(kRowTile);
-    least = kKeyTile;
+    least = c.dtype == MAFAT_BF16 ? 256 : 64;  // float32 products take eight times as long
   }
   int64_t n = (c.positions + least - 1) / least;
   if (n > want) n = want;

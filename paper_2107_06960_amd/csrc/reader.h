@@ -70,16 +70,22 @@ struct CrossArgs {
 // How a call is cut up, from its sizes alone (the workspace depends on it).
 struct CrossPlan {
   int splits;  // of the positions, joined afterwards
-  int few;     // 1: the kernel for few rows (bfloat16)
-  int waves;   // of the kernel for many rows (bfloat16): 32 rows each
+  int few;     // 1: cross_few_kernel
+  int waves;   // of cross_tile_kernel: 32 rows each
 };
 constexpr int kMaxCrossSplits = 64;  // one per lane of the joining wave
 CrossPlan plan_cross(const mafat_cross& c);
-// Waves of a block of the kernel for few rows, which share a split's positions.
-constexpr int cross_few_waves(int head_dim) { return head_dim <= 128 ? 4 : 2; }
+// Waves of a block of cross_few_kernel, which share a split's positions: so
+// many that their slots take 64 KB of LDS.
+constexpr int cross_few_waves(int dtype, int head_dim) {
+  const int row = head_dim * (dtype == MAFAT_F32 ? 4 : 2);
+  return row <= 256 ? 4 : 2;
+}
 // Blocks of `tile` rows of all frames together, at most.
 int64_t cross_row_blocks(const CrossArgs& a, int tile);
 hipError_t launch_cross(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
+// Whole 16-byte pieces; in float32 heads up to 128.
 hipError_t launch_cross_bf16(const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
+hipError_t launch_cross_f32(const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
 
 }  // namespace mafat
