@@ -51,7 +51,9 @@ __device__ __forceinline__ void load_to_lds(const u32x4& range, unsigned off, un
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(range[i])));
   to = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  // (The load needs five wait states after a vector instruction that wrote its
+  // descriptor, which the compiler does not count into assembly.)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(to), "v"(off), "s"(r)
                : "memory");
@@ -499,6 +501,7 @@ __global__ __launch_bounds__(64 * cross_few_waves(DT, DP), 1) void cross_few_ker
     return first_bits(at.keys - t * KT) & 0xffffffffu;
   };
   auto issue = [&](int t, uint64_t ok) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot's last reads are done
     const unsigned slot = base + (t & (SLOTS - 1)) * 2 * HALF;
     fk.template issue<false>(t, slot, 0, 0);
     fv.template issue<MASK == MASK_KEYS>(t, slot + HALF, 0, ok);
