@@ -367,7 +367,8 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tile_kernel(const LinearA
   // Epilogue: a lane has, for each of its rows (32 m + c), columns 8 j + 4 q
   // .. + 3 of every 32.  The adapters' products are added on the matrix cores,
   // u as the sum of two bfloat16 parts (16 bits, below the output's 8), one
-  // adapter of the 32 rows after another; a lane takes what belongs to its row.
+  // adapter of 32 rows after another, right before these rows leave, so that only
+  // their sums are in use beside the operands; a lane takes what belongs to its row.
   // Each wave turns its 32 rows of outputs round in LDS, so that they leave as
   // whole lines.
   constexpr int WCOLS = BN / WN;             // columns of a wave
@@ -396,60 +397,53 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tile_kernel(const LinearA
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[n][m][4 * g + i] = fmaf(acc[n][m][4 * g + i], sx[m] * sc[i], bi[i]);
     }
-  if constexpr (ADAPT) {
-    // One adapter of the wave's rows after another: its matrix is read once for all of them.
-    const uint16_t* const u = a.u + m0 * 2 * a.rank_pad;
-    int b_row[NT], u_row[MT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) b_row[n] = min(n0 + col0 + 32 * n + c, a.out_cols - 1) * a.rank + 8 * q;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) u_row[m] = min(wm * (BM / WM) + 32 * m + c, rows_m - 1) * 2 * a.rank_pad + 8 * q;
-    while (true) {
-      int ad = -1;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const uint64_t todo = __builtin_amdgcn_ballot_w64(mine[m] >= 0);
-        if (ad < 0 && todo) ad = __builtin_amdgcn_readlane(mine[m], __ffsll(static_cast<unsigned long long>(todo)) - 1);
-      }
-      if (ad < 0) break;
-      const uint16_t* const b = a.b + static_cast<int64_t>(ad) * a.out_cols * a.rank;
-      for (int r0 = 0; r0 < a.rank; r0 += 16) {
-        u32x4 bf[NT], up[MT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) bf[n] = load_rank8(b + b_row[n] + r0, a.rank - r0 - 8 * q);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          up[m][0] = up[m][1] = u32x4{0, 0, 0, 0};
-          if (mine[m] == ad) {
-            __builtin_memcpy(&up[m][0], u + u_row[m] + r0, 16);
-            __builtin_memcpy(&up[m][1], u + u_row[m] + a.rank_pad + r0, 16);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);  // all of these loads before the first use
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint64_t ours = __builtin_amdgcn_ballot_w64(mine[m] == ad);
-          if (!ours) continue;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            f32x16 sum = acc[n][m];
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-              sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bf[n]), __builtin_bit_cast(bf16x8, up[m][p]),
-                                                            sum, 0, 0, 0);
-            // rows of other adapters keep what they have, whatever this one's matrix holds
-            const bool keep = mine[m] != ad;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[n][m][i] = keep ? acc[n][m][i] : sum[i];
-          }
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) mine[m] = mine[m] == ad ? -1 : mine[m];
-    }
-  }
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
+    if constexpr (ADAPT) {
+      // One adapter of these 32 rows after another, 32 of its ranks at a time.
+      const uint16_t* const u = a.u + (m0 + min(wm * (BM / WM) + 32 * m + c, rows_m - 1)) * 2 * a.rank_pad + 8 * q;
+      uint64_t todo = __builtin_amdgcn_ballot_w64(mine[m] >= 0);
+#pragma unroll 1
+      while (todo) {
+        const int ad = __builtin_amdgcn_readlane(mine[m], __ffsll(static_cast<unsigned long long>(todo)) - 1);
+        const bool ours = mine[m] == ad;
+        todo &= ~__builtin_amdgcn_ballot_w64(ours);
+        const uint16_t* const b = a.b + static_cast<int64_t>(ad) * a.out_cols * a.rank + 8 * q;
+#pragma unroll 1
+        for (int r0 = 0; r0 < a.rank; r0 += 32) {
+          u32x4 bf[2][NT], up[2][2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int r = r0 + 16 * t;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              bf[t][n] = load_rank8(b + min(n0 + col0 + 32 * n + c, a.out_cols - 1) * a.rank + r, a.rank - r - 8 * q);
+            up[t][0] = up[t][1] = u32x4{0, 0, 0, 0};
+            if (ours && r < a.rank) {
+              __builtin_memcpy(&up[t][0], u + r, 16);
+              __builtin_memcpy(&up[t][1], u + a.rank_pad + r, 16);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            f32x16 sum;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (r0 + 16 * t >= a.rank) break;
+#pragma unroll
+              for (int p = 0; p < 2; ++p)
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bf[t][n]), __builtin_bit_cast(bf16x8, up[t][p]),
+                                                              sum, 0, 0, 0);
+            }
+            // rows of other adapters keep what they have, whatever this one's matrix holds
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][m][i] += ours ? sum[i] : 0.f;
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -676,13 +670,8 @@ hipError_t launch_shrink(const LinearArgs& a, hipStream_t stream) {
 template <int BN, int BM, int WN, int WM, int SLOTS>
 void launch_tile(const LinearArgs& a, int tn, int tm, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(tn) * static_cast<unsigned>(tm)), block(64 * WN * WM);
-  if constexpr (BN < 256) {  // the largest tiles are for calls without adapters
-    if (a.count) {
-      hipLaunchKernelGGL((linear_tile_kernel<BN, BM, WN, WM, SLOTS, true>), grid, block, 0, stream, a, tn, tm);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((linear_tile_kernel<BN, BM, WN, WM, SLOTS, false>), grid, block, 0, stream, a, tn, tm);
+  if (a.count) hipLaunchKernelGGL((linear_tile_kernel<BN, BM, WN, WM, SLOTS, true>), grid, block, 0, stream, a, tn, tm);
+  else hipLaunchKernelGGL((linear_tile_kernel<BN, BM, WN, WM, SLOTS, false>), grid, block, 0, stream, a, tn, tm);
 }
 
 template <int MT>
@@ -699,11 +688,11 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
   }
   const bool pieces = a.in_cols % 16 == 0 && whole(a.x, a.x_stride) && whole(a.w, a.w_stride);
   // More rows than linear_few_kernel takes at a time: tiles, as large as leaves
-  // a block for every CU; the largest without adapters only, whose code does
-  // not fit its registers.
+  // a block for every CU (8192 rows of 4096 by 4096, 8 adapters of rank 32: 131 us
+  // by tiles of 256, 140 by tiles of 128; without adapters 111).
   if (pieces && a.rows > 64) {
     const auto tiles = [&](int64_t n, int64_t m) { return ((a.out_cols + n - 1) / n) * ((a.rows + m - 1) / m); };
-    const int side = !a.count && tiles(256, 256) >= 256 ? 256 : tiles(128, 128) >= 256 ? 128 : 64;
+    const int side = tiles(256, 256) >= 256 ? 256 : tiles(128, 128) >= 256 ? 128 : 64;
     if (tiles(side, side) >= (int64_t{1} << 31)) return hipErrorInvalidValue;
     const int tn = (a.out_cols + side - 1) / side, tm = static_cast<int>((a.rows + side - 1) / side);
     if (side == 256) launch_tile<256, 256, 4, 2, 2>(a, tn, tm, stream);
