@@ -190,8 +190,6 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
       if (!d.a || !d.b || !d.of_row) return fail(MAFAT_EINVAL, "adapters: a, b and of_row must be non-NULL");
       if (!aligned(d.a, 2) || !aligned(d.b, 2) || !aligned(d.factor, 4) || !aligned(d.of_row, 4))
         return fail(MAFAT_EINVAL, "adapters: a pointer is not aligned to its elements");
-      if (ws_bytes < need)
-        return fail(MAFAT_EWORKSPACE, "workspace " + std::to_string(ws_bytes) + " < " + std::to_string(need) + " bytes");
       if (!workspace || !aligned(workspace, 256))
         return fail(MAFAT_EINVAL, "workspace must be non-NULL and 256-byte aligned");
       const int64_t an = 2 * static_cast<int64_t>(d.count) * d.rank * in_cols, bn = 2 * static_cast<int64_t>(d.count) * d.rank * out_cols;
@@ -203,6 +201,8 @@ extern "C" int mafat_linear(int64_t rows, int64_t in_cols, int64_t out_cols, con
       for (const Span& o : others)
         if (overlap(sy, o) || overlap(su, o)) return fail(MAFAT_EINVAL, "y or the workspace overlaps an input");
       if (overlap(sy, su)) return fail(MAFAT_EINVAL, "y overlaps the workspace");
+      if (ws_bytes < need)
+        return fail(MAFAT_EWORKSPACE, "workspace " + std::to_string(ws_bytes) + " < " + std::to_string(need) + " bytes");
       a.a = static_cast<const uint16_t*>(d.a);
       a.b = static_cast<const uint16_t*>(d.b);
       a.factor = d.factor;
