@@ -378,9 +378,9 @@ struct Fetch {
 // Per 64 keys a wave spends 1024 cycles in matrix instructions (DP 128) and
 // about as many on the vector ALUs, a third of them in the exponentials; its LDS
 // reads take 128.  The largest score lags (kLazy), so the sums are seldom
-// rescaled.  2 frames x 2048 rows x 16 heads of 128, 5776 positions: 202 us,
-// 960 TFLOP/s, four fifths of what a large bfloat16 product of the library
-// reaches on the same card, whose clocks both bring down.
+// rescaled.  2 frames x 2048 rows x 16 heads of 128, 5776 positions: 197 us,
+// 985 TFLOP/s, where a large bfloat16 product of the library reaches 1590; matrix
+// instructions are busy 38 % of the time, at a clock that both bring down to 2.0 GHz.
 template <int DT, int DP, int MASK, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs a) {
   using F = Fast<DT, DP>;
@@ -463,8 +463,9 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
 // another before the end, where the parts are joined in LDS.  The slots of a
 // block take at most 67 KB, so that two blocks share a CU: their waves fetch
 // while others compute, and a ragged call's blocks run in one round (8 frames,
-// 64 rows, 8 heads of 128, up to 1444 positions: 13.8 us; with twice the slots
-// and one block a CU 17.8).
+// 64 rows, 8 heads of 128, up to 1444 positions: 11.7 us and
+// 3.9 for the join; 4 rows, 64980 positions, 4 heads of 128 for 16: 97 us, 5.5 TB/s,
+// the rate of a copy).
 template <int DT, int DP, int MASK>
 __global__ __launch_bounds__(64 * cross_few_waves(DT, DP), 1) void cross_few_kernel(const CrossArgs a) {
   using F = Fast<DT, DP>;

@@ -140,7 +140,7 @@ struct FewOutputs {
 // Bound by reading the weights, once; every row of x is read by every block,
 // from the caches.  (Fragments read straight into registers take a line of the
 // first-level cache per lane, 69 accesses a load: 11.8 us for 64 rows of 4096
-// by 4096, that cache's rate.)  Operands as for the tiles below.
+// by 4096, that cache's rate; this one 7.4.)  Operands as for the tiles below.
 constexpr int few_waves(int mt) { return mt == 4 ? 4 : 8; }
 template <int MT>
 __global__ __launch_bounds__(64 * few_waves(MT)) void linear_few_kernel(const LinearArgs a) {
@@ -255,7 +255,8 @@ __device__ __forceinline__ void mma8_32(f32x16& c, const i32x8& a, const i32x8& 
 // p ^ (row / 2 % 8), so that the 16 lanes that are served at a time find
 // their pieces in 16 different places of the banks.  A lane takes pieces q and
 // q + 2 of a 64-byte half (q its half of the wave) for both operands.
-// Operands, strides and in_cols in multiples of 16 bytes.
+// Operands, strides and in_cols in multiples of 16 bytes.  8192 rows of 4096 by
+// 4096 without adapters: 111 us, 2.5 PFLOP/s (the library's 8-bit product 104).
 constexpr int kStage = 128;
 template <int BN, int BM, int WN, int WM, int SLOTS, bool ADAPT>
 __global__ __launch_bounds__(64 * WN * WM) void linear_tile_kernel(const LinearArgs a, int tiles_n, int tiles_m) {

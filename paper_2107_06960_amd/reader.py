@@ -64,7 +64,7 @@ class Reader:
         return kv[:, :, 0], kv[:, :, 1]
 
     def run(self, tokens, y, q_offsets=None, row_adapter=None, k_lengths=None, key_mask=None):
-        """tokens: [rows, width] in y's type, frame by frame; q_offsets: int32 [frames + 1], the frames' rows (None: as many
+        """tokens: bfloat16 [rows, width], as y has to be, frame by frame; q_offsets: int32 [frames + 1], the frames' rows (None: as many
         each); row_adapter: int32 [rows], the adapter of each row's request.  Returns the normed rows."""
         k, v = self.states(y)
         rows, h, delta = tokens.shape[0], tokens, None
