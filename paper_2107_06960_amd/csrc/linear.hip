@@ -70,22 +70,6 @@ __device__ __forceinline__ u32x4 load_rank8(const uint16_t* p, int n) {
   }
   return v;
 }
-// sum_r u[r] b[r] of one output column; u as its two parts, `pad` apart.
-__device__ __forceinline__ float expand(const uint16_t* u, int pad, const uint16_t* b, int rank) {
-  float s = 0.f;
-  for (int r = 0; r < rank; r += 8) {
-    uint16_t hi[8], lo[8];
-    __builtin_memcpy(hi, u + r, 16);
-    __builtin_memcpy(lo, u + pad + r, 16);
-    const u32x4 bv = load_rank8(b + r, rank - r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t w = bv[i >> 1];
-      s = fmaf(to_f(hi[i]) + to_f(lo[i]), __uint_as_float((i & 1) ? w & 0xffff0000u : w << 16), s);
-    }
-  }
-  return s;
-}
 // v as the sum of two bfloat16 parts (16 bits of it), to u and `pad` further on.
 __device__ __forceinline__ void put_parts(uint16_t* u, int pad, float v) {
   const __bf16 hi = static_cast<__bf16>(v);
@@ -102,21 +86,51 @@ struct FewOutputs {
   static constexpr int STEPS = (256 * MT + 64 * NW - 1) / (64 * NW);
   float scale[STEPS], add[STEPS];
   __device__ __forceinline__ void start(const LinearArgs& a, int n0, int64_t m0) {
+    int ad[STEPS];
+    float bias[STEPS];
+    // places past the end repeat the last row or column; what they get is not stored
+    const auto place = [&](int k, int64_t* m, int* j) {
+      const int e = static_cast<int>(threadIdx.x) + 64 * NW * k;
+      *m = min(m0 + (e >> 4), a.rows - 1);
+      *j = min(n0 + (e & 15), a.out_cols - 1);
+    };
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
-      const int e = static_cast<int>(threadIdx.x) + 64 * NW * k;
-      const int64_t m = m0 + (e >> 4);
-      const int j = n0 + (e & 15);
-      scale[k] = add[k] = 0.f;
-      if (e >= 256 * MT || m >= a.rows || j >= a.out_cols) continue;
+      int64_t m;
+      int j;
+      place(k, &m, &j);
+      ad[k] = a.count ? a.of_row[m] : -1;
       scale[k] = a.x_scale[m] * a.w_scale[j];
-      if (a.bias) add[k] = a.bias[j];
-      if (a.count) {
-        const int ad = a.of_row[m];
-        if (ad >= 0 && ad < a.count)
-          add[k] += expand(a.u + m * 2 * a.rank_pad, a.rank_pad, a.b + (static_cast<int64_t>(ad) * a.out_cols + j) * a.rank, a.rank);
-      }
+      bias[k] = a.bias ? a.bias[j] : 0.f;
+      add[k] = 0.f;
     }
+    // sum_r u[r] b[r]: of eight ranks, everything for all places before its first use
+    for (int r = 0; a.count && r < a.rank; r += 8) {
+      u32x4 hi[STEPS], lo[STEPS], bv[STEPS];
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        int64_t m;
+        int j;
+        place(k, &m, &j);
+        hi[k] = lo[k] = bv[k] = u32x4{0, 0, 0, 0};
+        if (ad[k] >= 0 && ad[k] < a.count) {
+          const uint16_t* u = a.u + m * 2 * a.rank_pad + r;
+          __builtin_memcpy(&hi[k], u, 16);
+          __builtin_memcpy(&lo[k], u + a.rank_pad, 16);
+          bv[k] = load_rank8(a.b + (static_cast<int64_t>(ad[k]) * a.out_cols + j) * a.rank + r, a.rank - r);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const auto part = [&](const u32x4& v) { return __uint_as_float((i & 1) ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); };
+          add[k] = fmaf(part(hi[k]) + part(lo[k]), part(bv[k]), add[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) add[k] = bias[k] + add[k];
   }
   // part: the waves' sums, by register and lane of the matrix instruction.
   __device__ __forceinline__ void finish(const LinearArgs& a, const f32x4 (*part)[MT][64], int n0, int64_t m0) const {
