@@ -246,7 +246,8 @@ def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_
     bfloat16; q_heads a multiple of kv_heads, d up to 256.  q_offsets: int32 [frames + 1], frame f's rows are q_offsets[f]
     to q_offsets[f + 1] (None: rows / frames each; rows that no frame has come back undefined).  k_lengths: int32
     [frames], the valid positions of each (None: all).  key_mask: bool [frames, positions] or row_mask: bool [rows,
-    positions], true where a position may be read.  scale: of q . k (None: 1 / sqrt(d)).  lse=True: the logarithm of each
+    positions], true where a position may be read.  scale: of q . k, a number (a tensor of one value is read on the host
+    at every call; None: 1 / sqrt(d)).  lse=True: the logarithm of each
     row's sum of exponentials, float32 [rows, q_heads], -inf for rows without any position (their y is 0); else None.
     """
     dt = q.dtype
@@ -268,6 +269,8 @@ def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_
         m_row = _row_stride(mask, "the mask") if positions else 0
     offsets_at = _vector(q_offsets, frames + 1, torch.int32, dev, "q_offsets")
     lengths_at = _vector(k_lengths, frames, torch.int32, dev, "k_lengths")
+    if scale is not None:
+        scale = float(scale)  # of a tensor its value now: the shapes below are kept by what they hold
     ref, need, _ = _cross_shape(dt, rows, hq, d, frames, positions, hkv, q.stride(), k.stride(), v.stride(), scale, m_row, by_row)
     y = torch.empty((rows, hq, d), dtype=dt, device=dev)
     got = torch.empty((rows, hq), dtype=torch.float32, device=dev) if lse else None
