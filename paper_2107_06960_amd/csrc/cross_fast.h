@@ -138,7 +138,9 @@ struct Rows {
     // for masked keys and must not meet it).
     const uint32_t flip = a.scale < 0.f ? (DT == MAFAT_BF16 ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale == 0.f ? 0u : ~0u;
     scale = a.scale == 0.f ? 1.f : fabsf(a.scale);
-    lazy = kLazy / scale;
+    // Finite for any scale: plus infinity would make no product larger than a
+    // maximum of minus infinity, and the first key would not be taken for one.
+    lazy = fminf(kLazy / scale, 0x1.fffffep127f);
     const T* q = static_cast<const T*>(a.q) + row * a.q_row + static_cast<int64_t>(head) * a.q_head;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
