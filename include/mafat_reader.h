@@ -117,7 +117,10 @@ typedef struct {
  * positions s (s < k_lengths[f], and allowed by the mask):
  *   p_s = softmax_s(scale * q[i][h] . k[f][s][h'])
  *   y[i][h] = sum_s p_s v[f][s][h'],  lse[i][h] = log sum_s exp(scale * ...)
- * A row that no position is valid for gets y = 0 and lse = -infinity.  Keys
+ * A row that no position is valid for gets y = 0 and lse = -infinity.  Scores
+ * (scale times product) are float32: one that is -infinity has p = 0, also
+ * where a row has no other (y = 0 and lse = -infinity then), and one that is
+ * +infinity or NaN makes its row NaN.  Keys
  * and values of positions that are not valid for any row of a frame by its
  * length or its mask may hold anything, NaN included.
  *   q_offsets  int32[frames + 1], not decreasing, each clamped to [0, rows]:

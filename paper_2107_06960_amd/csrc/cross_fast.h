@@ -216,7 +216,9 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[n][i] *= down;
     }
-    const float base = most == kNone ? 0.f : most * scale;
+    // Past float32: minus infinity is no key yet (every exponential is zero),
+    // plus infinity makes the row NaN, as infinity minus infinity would.
+    const float high = most * scale, base = high == kNone ? 0.f : high + (high - high);
     float add = 0.f;
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub)
@@ -289,7 +291,7 @@ struct Rows {
   __device__ __forceinline__ void finish(const CrossArgs& a, int split, int n0, int step) {
     const int h = (static_cast<int>(threadIdx.x) & 63) >> 5, D = a.head_dim;
     if (!real) return;
-    const float top = most == kNone ? kNone : most * scale;
+    const float top = most * scale;
     if (a.splits > 1) {
       const int64_t pair = (static_cast<int64_t>(split) * a.rows + row) * a.q_heads + head;
       float* po = a.part + pair * D;

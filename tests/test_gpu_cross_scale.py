@@ -1,5 +1,7 @@
 """Scales of cross attention (mafat_cross_attention) at the ends of their range and between calls; bounds as in
 test_gpu_cross.py."""
+import math
+
 import pytest
 
 from gpu_util import require_gpu
@@ -29,3 +31,28 @@ def test_scales_near_zero(rows, s, scale, dtype):
     require_gpu()
     _check(_make(2, rows, s, 4, 2, 64, dtype, 7, ragged=True, mask="keys"), scale=scale)
     _check(_make(1, rows, s, 4, 2, 33, dtype, 7), scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 33])
+@pytest.mark.parametrize("rows, s", [(6, 150), (6, 3000), (200, 150), (200, 3000)])
+def test_scores_past_float32(rows, s, d, dtype):
+    """Products within float32 that the scale takes past it: NaN above, and below as if not valid; the other rows as ever."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    a = _make(1, rows, s, 2, 1, d, dtype, 5)
+    a["k"].abs_().add_(0.1)
+    small = a["q"].clone() * 1e-20
+    want, want_lse = O.cross_attention(small, a["k"], a["v"], scale=1e20, lse=True)
+    q = small.clone()
+    q[1], q[3] = 1e20, -1e20
+    y, lse = O.cross_attention(q, a["k"], a["v"], scale=1e20, lse=True)
+    assert torch.isnan(y[1]).all() and torch.isnan(lse[1]).all()
+    assert not y[3].any() and (lse[3] == -math.inf).all()
+    others = [i for i in range(rows) if i not in (1, 3)]
+    assert torch.isfinite(want).all() and torch.isfinite(want_lse).all()
+    # rows of a wave rescale their sums together, so the last bits may differ
+    assert (y[others].float() - want[others].float()).abs().max() <= 2.0 ** -7
+    assert (lse[others] - want_lse[others]).abs().max() <= 2.0 ** -18 * want_lse.abs().max()
