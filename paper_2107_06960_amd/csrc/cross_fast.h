@@ -90,8 +90,9 @@ struct MaskBits {
     return bits;
   }
   __device__ __forceinline__ void fill(const unsigned char* mask, int from, int keys) {
-    const int at = from + 64 * (static_cast<int>(threadIdx.x) & 63);
-    mine = at < keys && at >= from ? of(mask + at, keys - at) : 0;
+    // (unsigned: a span may look past 2^31 positions)
+    const uint32_t at = static_cast<uint32_t>(from) + 64 * (threadIdx.x & 63), all = static_cast<uint32_t>(keys);
+    mine = at < all ? of(mask + at, static_cast<int>(all - at)) : 0;
   }
   // Of 64 positions from 64 g after the first.
   __device__ __forceinline__ uint64_t get(int g) const {
