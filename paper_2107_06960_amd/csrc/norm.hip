@@ -261,17 +261,41 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
   }
 }
 
+// A launch has fewer than 2^32 threads: where a row per block would pass
+// that, `most` rows after another go in a launch of their own.
+template <int DT, int OUT, typename F>
+hipError_t by_rows(const NormArgs& a, int64_t most, F launch_rows) {
+  using T = typename Elt<DT>::T;
+  using Y = typename OutElt<OUT>::T;
+  for (int64_t at = 0; at < a.rows; at += most) {
+    NormArgs p = a;
+    p.rows = a.rows - at < most ? a.rows - at : most;
+    p.x = static_cast<const T*>(a.x) + at * a.x_stride;
+    if (a.res) {
+      p.res = static_cast<const T*>(a.res) + at * a.res_stride;
+      p.sum = static_cast<T*>(a.sum) + at * a.sum_stride;
+    }
+    p.y = static_cast<Y*>(a.y) + at * a.y_stride;
+    if (a.y_scale) p.y_scale = a.y_scale + at;
+    launch_rows(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int DT, int OUT, bool RES>
 hipError_t launch(const NormArgs& a, hipStream_t stream) {
   constexpr int V = Piece<DT>::V;
+  constexpr int64_t kThreads = int64_t{1} << 31;  // of a launch, at most
   const int64_t pieces = (static_cast<int64_t>(a.cols) + V - 1) / V;
 #define MAFAT_NORM(team_, np_)                                                                               \
   do {                                                                                                       \
-    constexpr int teams = (team_) >= 256 ? 1 : 256 / (team_);                                                \
-    hipLaunchKernelGGL((norm_kernel<DT, OUT, RES, team_, np_>),                                              \
-                       dim3(static_cast<unsigned>((a.rows + teams - 1) / teams)),                            \
-                       dim3((team_) > 256 ? (team_) : 256), 0, stream, a);                                   \
-    return hipGetLastError();                                                                                \
+    constexpr int teams = (team_) >= 256 ? 1 : 256 / (team_), block = (team_) > 256 ? (team_) : 256;         \
+    return by_rows<DT, OUT>(a, teams * (kThreads / block), [&](const NormArgs& p) {                          \
+      hipLaunchKernelGGL((norm_kernel<DT, OUT, RES, team_, np_>),                                            \
+                         dim3(static_cast<unsigned>((p.rows + teams - 1) / teams)), dim3(block), 0, stream, p); \
+    });                                                                                                      \
   } while (0)
   if (pieces <= 16) MAFAT_NORM(16, 1);
   if (pieces <= 64) MAFAT_NORM(64, 1);
@@ -282,8 +306,9 @@ hipError_t launch(const NormArgs& a, hipStream_t stream) {
   if (pieces <= 2048) MAFAT_NORM(1024, 2);
   if (pieces <= 4096) MAFAT_NORM(1024, 4);
 #undef MAFAT_NORM
-  hipLaunchKernelGGL((norm_long_kernel<DT, OUT, RES>), dim3(static_cast<unsigned>(a.rows)), dim3(1024), 0, stream, a);
-  return hipGetLastError();
+  return by_rows<DT, OUT>(a, kThreads / 1024, [&](const NormArgs& p) {
+    hipLaunchKernelGGL((norm_long_kernel<DT, OUT, RES>), dim3(static_cast<unsigned>(p.rows)), dim3(1024), 0, stream, p);
+  });
 }
 
 template <int DT, int OUT>

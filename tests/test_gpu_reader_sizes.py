@@ -33,3 +33,27 @@ def test_a_key_mask_up_to_the_last_position_there_can_be(rows):
     y, allowed, want_lse, lse_allowed = _formula({"q": q, "k": k[:, at], "v": k[:, at]})
     assert torch.all((got.double().cpu() - y).abs() <= allowed)
     assert torch.all((lse.double().cpu() - want_lse).abs() <= lse_allowed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype, rows, cols, residual", [("f32", 2 ** 28 + 9, 1, True), ("bf16", 2 ** 26 + 5, 129, False),
+                                                         ("bf16", 2 ** 24 + 3, 1025, False), ("bf16", 2 ** 22 + 3, 8200, False)])
+def test_norm_of_rows_past_a_launch(dtype, rows, cols, residual):
+    """Each number of threads per row with 2^32 threads and a few blocks more; all rows but a few are zeros."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x = torch.zeros(rows, cols, dtype=dt, device="cuda")
+    at = torch.tensor([0, 1, rows // 2 - 1, rows // 2, rows - 12, rows - 2, rows - 1], device="cuda")
+    torch.manual_seed(cols)
+    x[at] = torch.randn(len(at), cols, device="cuda").to(dt)
+    r = torch.ones(rows, cols, dtype=dt, device="cuda") if residual else None
+    h, y, scale = O.add_rms_norm(x, None, r)
+    small = O.add_rms_norm(x[at], None, r[at] if residual else None)
+    assert torch.equal(y[at].view(torch.uint8), small[1].view(torch.uint8)) and torch.equal(scale[at], small[2])
+    if residual:
+        assert torch.equal(h[at], small[0]) and int((h == 1).sum()) == rows - len(at)
+    rest = 1 / 448 if residual else 1.0  # the scale of a row of ones, of a row of zeros
+    near = ((scale - rest).abs() < 1e-6).sum() - ((small[2] - rest).abs() < 1e-6).sum()
+    assert int(near) == rows - len(at)
