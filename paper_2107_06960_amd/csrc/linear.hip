@@ -694,9 +694,13 @@ void launch_few(const LinearArgs& a, dim3 grid, hipStream_t stream) {
   hipLaunchKernelGGL(linear_few_kernel<MT>, grid, dim3(64 * few_waves(MT)), 0, stream, a);
 }
 
-}  // namespace
+// Rows of one launch of each kernel, at most: it has fewer than 2^32 threads
+// along the grid's first axis (shrink_rows_kernel has 256 a row) and 65535
+// blocks of linear_any_kernel's 64 rows along its second.  Whole row tiles.
+constexpr int64_t kLaunchRows = (int64_t{1} << 22) - 256;
+static_assert(kLaunchRows <= int64_t{65535} * 16 * kAnyTiles && kLaunchRows % 256 == 0, "rows of a launch");
 
-hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
+hipError_t launch_rows(const LinearArgs& a, hipStream_t stream) {
   if (a.count) {
     const hipError_t e = launch_shrink(a, stream);
     if (e != hipSuccess) return e;
@@ -708,7 +712,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
   if (pieces && a.rows > 64) {
     const auto tiles = [&](int64_t n, int64_t m) { return ((a.out_cols + n - 1) / n) * ((a.rows + m - 1) / m); };
     const int side = tiles(256, 256) >= 256 ? 256 : tiles(128, 128) >= 256 ? 128 : 64;
-    if (tiles(side, side) >= (int64_t{1} << 31)) return hipErrorInvalidValue;
+    if (tiles(side, side) >= (int64_t{1} << 23)) return hipErrorInvalidValue;  // 512 threads each (y would take a TB)
     const int tn = (a.out_cols + side - 1) / side, tm = static_cast<int>((a.rows + side - 1) / side);
     if (side == 256) launch_tile<256, 256, 4, 2, 2>(a, tn, tm, stream);
     else if (side == 128) launch_tile<128, 128, 2, 2, 2>(a, tn, tm, stream);
@@ -722,11 +726,17 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
     else launch_few<4>(a, dim3(nt), stream);
     return hipGetLastError();
   }
-  // the grid's second axis ends at 65535: more rows go in several launches
-  constexpr int64_t kRows = int64_t{65535} * 16 * kAnyTiles;
-  for (int64_t at = 0; at < a.rows; at += kRows) {
+  const dim3 grid(nt, static_cast<unsigned>((a.rows + 16 * kAnyTiles - 1) / (16 * kAnyTiles)));
+  hipLaunchKernelGGL(linear_any_kernel, grid, dim3(64 * kAnyWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
+  for (int64_t at = 0; at < a.rows; at += kLaunchRows) {
     LinearArgs p = a;
-    p.rows = a.rows - at < kRows ? a.rows - at : kRows;
+    p.rows = a.rows - at < kLaunchRows ? a.rows - at : kLaunchRows;
     p.x = a.x + at * a.x_stride;
     p.x_scale = a.x_scale + at;
     p.y = static_cast<uint16_t*>(a.y) + at * a.y_stride;
@@ -734,9 +744,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
       p.of_row = a.of_row + at;
       p.u = a.u + at * 2 * a.rank_pad;
     }
-    const dim3 grid(nt, static_cast<unsigned>((p.rows + 16 * kAnyTiles - 1) / (16 * kAnyTiles)));
-    hipLaunchKernelGGL(linear_any_kernel, grid, dim3(64 * kAnyWaves), 0, stream, p);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_rows(p, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -57,3 +57,27 @@ def test_norm_of_rows_past_a_launch(dtype, rows, cols, residual):
     rest = 1 / 448 if residual else 1.0  # the scale of a row of ones, of a row of zeros
     near = ((scale - rest).abs() < 1e-6).sum() - ((small[2] - rest).abs() < 1e-6).sum()
     assert int(near) == rows - len(at)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows, k, n, adapters", [(2 ** 24 + 5, 17, 3, 2), (2 ** 29 + 37, 16, 1, 1), (2 ** 31 - 1, 16, 1, 0)])
+def test_linear_of_rows_past_a_launch(rows, k, n, adapters):
+    """Each way of the adapters' inner products, and the tiles, with 2^32 threads and more; all rows but a few are zeros."""
+    require_gpu()
+    import torch
+    import test_gpu_linear as L
+    from paper_2107_06960_amd import operators as O
+    at = torch.tensor([0, 1, 2 ** 22 - 257, 2 ** 22 - 256, rows // 2, rows - 40, rows - 2, rows - 1], device="cuda")
+    sx, sxs, w, ws, bias, ad, of = L._make(len(at), k, n, adapters, 3, k)
+    x = torch.zeros(rows, k, dtype=torch.uint8, device="cuda")
+    x[at] = sx.contiguous().view(torch.uint8)
+    xs = torch.ones(rows, device="cuda")
+    xs[at] = sxs
+    of_row = None
+    if adapters:
+        of_row = torch.full((rows,), adapters - 1, dtype=torch.int32, device="cuda")
+        of_row[at] = of
+    y = O.linear8(x.view(O.F8), xs, w, ws, bias, ad, of_row)
+    L._check(y[at], (sx, sxs, w, ws, bias, ad, of))
+    for j in range(n):  # zeros give the bias
+        assert rows - len(at) <= int((y[:, j] == bias[j].bfloat16()).sum()) <= rows
