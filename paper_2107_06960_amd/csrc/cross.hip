@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
   unsigned char* const sv = smem + kKeyTile * PITCH;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int c = lane & 31, h = lane >> 5;
-  const Place at = find<kRowTile>(a, static_cast<int>(blockIdx.x));
+  const Place at = find<kRowTile>(a, a.first_block + static_cast<int>(blockIdx.x));
   if (!at.any) return;
   const int head0 = static_cast<int>(blockIdx.y) * a.group;
   const int split = static_cast<int>(blockIdx.z);
@@ -349,12 +349,15 @@ hipError_t launch(const CrossArgs& a, const CrossPlan& p, hipStream_t stream) {
   } else {
     const int64_t blocks = cross_row_blocks(a, kRowTile);
     if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits));
-    if (a.head_dim <= 64) launch_any<DT, 64>(a, grid, stream);
-    else if (a.head_dim <= 96) launch_any<DT, 96>(a, grid, stream);
-    else if (a.head_dim <= 128) launch_any<DT, 128>(a, grid, stream);
-    else launch_any<DT, 256>(a, grid, stream);
-    e = hipGetLastError();
+    e = for_block_parts(blocks, [&](int32_t from, unsigned n) {
+      CrossArgs p = a;
+      p.first_block = from;
+      const dim3 grid(n, static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits));
+      if (a.head_dim <= 64) launch_any<DT, 64>(p, grid, stream);
+      else if (a.head_dim <= 96) launch_any<DT, 96>(p, grid, stream);
+      else if (a.head_dim <= 128) launch_any<DT, 128>(p, grid, stream);
+      else launch_any<DT, 256>(p, grid, stream);
+    });
   }
   if (e != hipSuccess || a.splits == 1) return e;
   const unsigned pairs = static_cast<unsigned>(a.rows) * static_cast<unsigned>(a.q_heads);

@@ -396,7 +396,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
   __shared__ __align__(1024) unsigned char smem[4 * HALF];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   // head by head, so that the blocks that share keys and values share an XCD's cache
-  const int id = xcd_remap(static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
+  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
   const int kv = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.row_blocks));
   const Place at = find<32 * NW>(a, id - kv * a.row_blocks);
   if (!at.any) return;
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(64 * cross_few_waves(DT, DP), 1) void cross_few_ker
   __shared__ __align__(1024) unsigned char smem[LDS];
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int id = xcd_remap(static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
+  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.row_blocks * a.kv_heads);
   const int kv = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.row_blocks));
   const Place at = find<32>(a, id - kv * a.row_blocks);
   if (!at.any) return;
@@ -602,17 +602,19 @@ template <int DT, int DP>
 hipError_t launch_fast(CrossArgs a, const CrossPlan& p, hipStream_t stream) {
   constexpr int FEW = 64 * cross_few_waves(DT, DP);
   a.row_blocks = static_cast<int32_t>(cross_row_blocks(a, p.few ? 32 : 32 * p.waves));
-  const dim3 grid(static_cast<unsigned>(a.row_blocks) * static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits));
-  if (p.few) {
-    if (!a.mask) hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_NONE>), grid, dim3(FEW), 0, stream, a);
-    else if (!a.mask_by_row) hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_KEYS>), grid, dim3(FEW), 0, stream, a);
-    else hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_ROWS>), grid, dim3(FEW), 0, stream, a);
-  } else if (DP > 128 || p.waves == 8) {
-    launch_tile<DT, DP, 8>(a, grid, stream);
-  } else {
-    launch_tile<DT, DP <= 128 ? DP : 128, 4>(a, grid, stream);
-  }
-  return hipGetLastError();
+  return for_block_parts(static_cast<int64_t>(a.row_blocks) * a.kv_heads, [&](int32_t from, unsigned n) {
+    a.first_block = from;
+    const dim3 grid(n, static_cast<unsigned>(a.splits));
+    if (p.few) {
+      if (!a.mask) hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_NONE>), grid, dim3(FEW), 0, stream, a);
+      else if (!a.mask_by_row) hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_KEYS>), grid, dim3(FEW), 0, stream, a);
+      else hipLaunchKernelGGL((cross_few_kernel<DT, DP, MASK_ROWS>), grid, dim3(FEW), 0, stream, a);
+    } else if (DP > 128 || p.waves == 8) {
+      launch_tile<DT, DP, 8>(a, grid, stream);
+    } else {
+      launch_tile<DT, DP <= 128 ? DP : 128, 4>(a, grid, stream);
+    }
+  });
 }
 
 }  // namespace

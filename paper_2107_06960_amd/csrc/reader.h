@@ -65,6 +65,7 @@ struct CrossArgs {
   int32_t splits;
   int32_t per_frame;   // query rows of a frame, without offsets
   int32_t row_blocks;  // blocks of query rows, of all frames together (at most)
+  int32_t first_block;  // of this launch (see for_block_parts)
   float scale;         // times log2(e): scores are in base 2
 };
 // How a call is cut up, from its sizes alone (the workspace depends on it).
@@ -80,6 +81,19 @@ CrossPlan plan_cross(const mafat_cross& c);
 constexpr int cross_few_waves(int dtype, int head_dim) {
   const int row = head_dim * (dtype == MAFAT_F32 ? 4 : 2);
   return row <= 256 ? 4 : 2;
+}
+// A launch has fewer than 2^32 threads along an axis of its grid: more blocks
+// than this along the first go in several, f(first block, blocks).  (A multiple
+// of 8, so that xcd_remap finds the blocks of a launch on the XCDs it expects.)
+constexpr int64_t kCrossLaunchBlocks = int64_t{1} << 22;
+template <typename F>
+hipError_t for_block_parts(int64_t blocks, F f) {
+  for (int64_t at = 0; at < blocks; at += kCrossLaunchBlocks) {
+    f(static_cast<int32_t>(at), static_cast<unsigned>(blocks - at < kCrossLaunchBlocks ? blocks - at : kCrossLaunchBlocks));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 // Blocks of `tile` rows of all frames together, at most.
 int64_t cross_row_blocks(const CrossArgs& a, int tile);

@@ -81,3 +81,18 @@ def test_linear_of_rows_past_a_launch(rows, k, n, adapters):
     L._check(y[at], (sx, sxs, w, ws, bias, ad, of))
     for j in range(n):  # zeros give the bias
         assert rows - len(at) <= int((y[:, j] == bias[j].bfloat16()).sum()) <= rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("frames, each, d", [(2 ** 24 + 3, 1, 8), (2 ** 24 + 3, 1, 7), (2 ** 23 + 1, 65, 8)])
+def test_cross_attention_of_frames_past_a_launch(frames, each, d):
+    """The kernels for few rows, for any size and for many rows with 2^32 threads and a few blocks more.  Frames of one
+    position: every row gets its frame's value as it is."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    torch.manual_seed(d)
+    v = torch.randn(frames, 1, 1, d, device="cuda").bfloat16()
+    q = torch.ones(frames * each, 1, d, dtype=torch.bfloat16, device="cuda")
+    y, _ = O.cross_attention(q, v, v)
+    assert torch.equal(y.view(frames, each, d), v.view(frames, 1, d).expand(frames, each, d))
