@@ -139,7 +139,8 @@ typedef struct {
  * (null or misaligned pointer, bad size or stride, rows not divisible without
  * q_offsets, scale not finite, y overlapping an input), EWORKSPACE,
  * EUNSUPPORTED (dtype, head_dim > 256, sizes of 2^31 or more, strides of 2^31
- * bytes or more), EHIP. */
+ * bytes or more, a scale above 2.35e38 either way, which overflows in base 2),
+ * EHIP. */
 int mafat_cross_workspace(const mafat_cross* c, size_t* bytes);
 int mafat_cross_attention(const mafat_cross* c, const void* q, const void* k, const void* v,
                           const int32_t* q_offsets, const int32_t* k_lengths, const unsigned char* mask,

@@ -68,6 +68,9 @@ int check_linear(int64_t rows, int64_t in_cols, int64_t out_cols, const mafat_ad
   return MAFAT_OK;
 }
 
+// What the kernels multiply products by: their exponentials are powers of two.
+float base2_scale(float scale) { return static_cast<float>(static_cast<double>(scale) * 1.4426950408889634); }
+
 // The sizes and strides of an attention call; the workspace holds the parts
 // that the splits of the positions are joined from.
 int check_cross(const mafat_cross* c, size_t* bytes) {
@@ -79,6 +82,7 @@ int check_cross(const mafat_cross* c, size_t* bytes) {
   if (c->head_dim < 1) return fail(MAFAT_EINVAL, "head_dim must be >= 1");
   if (c->head_dim > 256) return fail(MAFAT_EUNSUPPORTED, "head_dim above 256");
   if (!std::isfinite(c->scale)) return fail(MAFAT_EINVAL, "scale must be finite");
+  if (!std::isfinite(base2_scale(c->scale))) return fail(MAFAT_EUNSUPPORTED, "scale above 2.35e38");
   const int64_t d = c->head_dim;
   if (c->q_head < d || c->k_head < d || c->v_head < d || c->y_head < d)
     return fail(MAFAT_EINVAL, "a head stride is smaller than head_dim");
@@ -288,7 +292,7 @@ extern "C" int mafat_cross_attention(const mafat_cross* c, const void* q, const 
     a.per_frame = static_cast<int32_t>(c->rows / c->frames);
     const CrossPlan plan = plan_cross(*c);
     a.splits = plan.splits;
-    a.scale = static_cast<float>(static_cast<double>(c->scale) * 1.4426950408889634);
+    a.scale = base2_scale(c->scale);
     return launched(launch_cross(c->dtype, a, plan, static_cast<hipStream_t>(stream)), "cross attention");
   });
 }
