@@ -142,9 +142,8 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
         uint32_t pp[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+          add += s[2 * i] + s[2 * i + 1];  // as they are: the log-sum-exp is float32 whatever the second product takes
           pp[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
-          // the sum is that of the rounded values: what is divided is what was added up
-          add += __uint_as_float(pp[i] << 16) + __uint_as_float(pp[i] & 0xffff0000u);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
