@@ -134,8 +134,13 @@ typedef struct {
  *   y          [rows][q_heads][head_dim] in dtype;  lse float32 [rows][q_heads]
  *              contiguous, natural logarithm, or NULL
  *   workspace  mafat_cross_workspace bytes, 256-byte aligned (NULL if 0)
- * Softmax statistics and sums are float32; bfloat16 probabilities enter the
- * second product rounded to bfloat16, each by its own size.  Errors: EINVAL
+ * Softmax statistics and sums are float32.  In bfloat16 the exponentials enter
+ * the second product as the sum of two bfloat16 parts (16 bits) where a frame
+ * has up to 64 pairs of a row and a head that share a key/value head (rows /
+ * frames counted alike), or where head_dim, or an address or stride of k or v,
+ * is no multiple of 16 bytes; else rounded to bfloat16, each by its own size.
+ * So, and because rows of a wave rescale their sums together, the last bits of
+ * a row may depend on the rows that share its call.  Errors: EINVAL
  * (null or misaligned pointer, bad size or stride, rows not divisible without
  * q_offsets, scale not finite, y overlapping an input), EWORKSPACE,
  * EUNSUPPORTED (dtype, head_dim > 256, sizes of 2^31 or more, strides of 2^31

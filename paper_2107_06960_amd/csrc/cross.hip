@@ -139,11 +139,14 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
         s[i] = __builtin_amdgcn_exp2f(s[i] - base);
       }
       if constexpr (DT == MAFAT_BF16) {
-        uint32_t pp[8];
+        // Each exponential as the sum of two bfloat16 parts (see Rows in
+        // cross_fast.h): matrix instructions are not what this kernel waits for.
+        uint32_t pp[8], pl[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           add += s[2 * i] + s[2 * i + 1];  // as they are: the log-sum-exp is float32 whatever the second product takes
           pp[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
+          pl[i] = pack_bf16(s[2 * i] - __uint_as_float(pp[i] << 16), s[2 * i + 1] - __uint_as_float(pp[i] & 0xffff0000u));
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -169,6 +172,7 @@ __global__ __launch_bounds__(256) void cross_any_kernel(const CrossArgs a) {
             }
             const s16x4 vf[2] = {lo, hi};
             Tile<DT>::mul(acc[n], __builtin_bit_cast(u32x4, vf), u32x4{pp[4 * u], pp[4 * u + 1], pp[4 * u + 2], pp[4 * u + 3]});
+            Tile<DT>::mul(acc[n], __builtin_bit_cast(u32x4, vf), u32x4{pl[4 * u], pl[4 * u + 1], pl[4 * u + 2], pl[4 * u + 3]});
           }
         }
       } else {
