@@ -52,9 +52,11 @@ __device__ __forceinline__ void load_to_lds(const u32x4& range, unsigned off, un
   for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(range[i])));
   to = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
   // (The load needs five wait states after a vector instruction that wrote its
-  // descriptor, which the compiler does not count into assembly.)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
+  // descriptor, which the compiler does not count into assembly.  m0 is a
+  // register that assembly cannot declare as overwritten, so it is put back.)
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
                : "s"(to), "v"(off), "s"(r)
                : "memory");
 }

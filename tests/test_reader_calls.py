@@ -1,11 +1,26 @@
 """CPU tests of the reader's calls beside the refusals of test_reader_abi.py."""
 import ctypes
+import glob
+import os
+import re
 
 import pytest
 
 from paper_2107_06960_amd import mafat as M
 from paper_2107_06960_amd import operators as O
-from test_reader_abi import CROSS
+from test_reader_abi import CROSS, ROOT
+
+
+def test_assembly_puts_m0_back():
+    """The compiler may keep a value of its own in m0, and assembly cannot declare that register as overwritten."""
+    found = 0
+    for path in glob.glob(os.path.join(ROOT, "paper_2107_06960_amd", "csrc", "*")):
+        for text in re.findall(r"\basm\s+volatile\s*\((.*?)\);", open(path).read(), re.S):
+            if re.search(r"\bm0,", text):
+                found += 1
+                steps = [step.strip() for step in re.search(r'"(.*?)"\s*\n?\s*:', text, re.S).group(1).split(r"\n\t")]
+                assert steps[0] == "s_mov_b32 %0, m0" and steps[-1] == "s_mov_b32 m0, %0", (path, steps)
+    assert found
 
 
 @pytest.mark.parametrize("scale, status", [(2.35e38, 0), (-2.35e38, 0), (2.37e38, M.MAFAT_EUNSUPPORTED),
