@@ -4,7 +4,8 @@ maps that a ``mafat.Network`` leaves on the device.
 ``mafat_add_rms_norm``, ``mafat_linear`` and ``mafat_cross_attention`` keep the C names and only marshal arguments
 (device pointers and sizes).  ``add_rms_norm``, ``linear8`` and ``cross_attention`` take torch tensors on the GPU, check
 them, allocate what they return and run on the current stream of the tensors' device.  There is no fallback: every step
-runs in the library's HIP kernels.
+runs in the library's HIP kernels.  They are forward only: a tensor that requires a gradient is refused while gradients are
+recorded (call under torch.no_grad(), or pass it detached).
 """
 from __future__ import annotations
 
@@ -65,6 +66,7 @@ def lib():
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_recording = torch.is_grad_enabled
 
 
 def _call(name, index, *args):
@@ -89,6 +91,15 @@ def _ptr(t):
 
 def _refuse(text):
     raise ValueError(text)
+
+
+def _wants_grad(t):
+    return t is not None and t.requires_grad
+
+
+def _forward_only():
+    """Refuses what would come back without its gradient and without a word."""
+    _refuse("the operators are forward only: call them under torch.no_grad(), or on detached tensors")
 
 
 def _vector(t, n, dtype, dev, name):
@@ -171,6 +182,8 @@ def add_rms_norm(x, gain=None, residual=None, eps=1e-6, out="f8"):
     dt, to = x.dtype, _NAMES.get(out)
     if not x.is_cuda or x.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
         _refuse("x must be a float32 or bfloat16 matrix on the GPU")
+    if _recording() and (x.requires_grad or _wants_grad(gain) or _wants_grad(residual)):
+        _forward_only()
     if to is None:
         _refuse(f"out must be one of {sorted(_NAMES)}, not {out!r}")
     rows, cols = x.shape
@@ -205,6 +218,9 @@ def linear8(x, x_scale, w, w_scale, bias=None, adapters=None, row_adapter=None):
     """
     if not x.is_cuda or x.dim() != 2 or w.dim() != 2 or x.dtype is not F8:
         _refuse("x and w must be float8_e4m3fn matrices on the GPU")
+    if _recording() and (x.requires_grad or w.requires_grad or _wants_grad(x_scale) or _wants_grad(w_scale) or
+                         _wants_grad(bias) or (adapters is not None and any(map(_wants_grad, adapters)))):
+        _forward_only()
     rows, k = x.shape
     n, dev = w.shape[0], x.device
     if k < 1 or n < 1:
@@ -253,6 +269,8 @@ def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_
     dt = q.dtype
     if not q.is_cuda or q.dim() != 3 or (dt is not torch.bfloat16 and dt is not torch.float32):
         _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or getattr(scale, "requires_grad", False)):
+        _forward_only()
     rows, hq, d = q.shape
     dev, shape = q.device, k.shape
     if k.dim() != 4 or shape != v.shape or shape[3] != d or k.dtype is not dt or v.dtype is not dt or k.device != dev or \
