@@ -96,3 +96,80 @@ def test_cross_attention_of_frames_past_a_launch(frames, each, d):
     q = torch.ones(frames * each, 1, d, dtype=torch.bfloat16, device="cuda")
     y, _ = O.cross_attention(q, v, v)
     assert torch.equal(y.view(frames, each, d), v.view(frames, 1, d).expand(frames, each, d))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows, d, mask", [(3, 128, "keys"), (100, 128, "keys"), (3, 127, "keys"), (520, 128, "rows"),
+                                           (520, 127, "rows")])
+def test_frames_past_2_31_elements(rows, d, mask):
+    """The kernels for few rows, many rows and any size; keys and values of 2.2e9 elements in rows of 512, and masks of 2.2e9
+    bytes where a row has its own.  Read are some positions at the start, around 2^30 and 2^31 elements and at the end."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    s = 4_300_000
+    assert s * 512 > 2 ** 31
+    at = torch.cat([torch.arange(20), torch.arange(2 ** 21 - 20, 2 ** 21 + 20), torch.arange(2 ** 22 - 20, 2 ** 22 + 20),
+                    torch.arange(s - 200, s)]).cuda()
+    kv = torch.zeros(1, s, 2, 2, 128, dtype=torch.bfloat16, device="cuda")
+    torch.manual_seed(rows + d)
+    kv[:, at] = torch.randn(1, len(at), 2, 2, 128, device="cuda").bfloat16()
+    k, v = kv[:, :, 0, :, :d], kv[:, :, 1, :, :d]
+    q = torch.randn(rows, 2, d, device="cuda").bfloat16()
+    some = torch.rand(rows if mask == "rows" else 1, len(at), device="cuda") < 0.8
+    m = torch.zeros(len(some), s, dtype=torch.bool, device="cuda")
+    m[:, at] = some
+    name = {"keys": "key_mask", "rows": "row_mask"}[mask]
+    got, lse = O.cross_attention(q, k, v, lse=True, **{name: m})
+    pick = torch.tensor([0, 1, rows // 2, rows - 2, rows - 1], device="cuda").unique()
+    small = {"q": q[pick], "k": k[:, at], "v": v[:, at], name: some[pick] if mask == "rows" else some}
+    y, allowed, want_lse, lse_allowed = _formula(small)
+    assert torch.all((got[pick].double().cpu() - y).abs() <= allowed)
+    assert torch.all((lse[pick].double().cpu() - want_lse).abs() <= lse_allowed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [2048, 2047])
+def test_linear_past_2_31_elements(k):
+    """x and y of more than 2^31 elements each, on the tiles and on the kernel for any size."""
+    require_gpu()
+    import torch
+    import test_gpu_linear as L
+    from paper_2107_06960_amd import operators as O
+    rows, n = 1_100_000, 2000
+    assert rows * k > 2 ** 31 and rows * n > 2 ** 31
+    at = torch.cat([torch.arange(3), torch.arange(rows // 2, rows // 2 + 30), torch.arange(rows - 70, rows)]).cuda()
+    sx, sxs, w, ws, bias, ad, of = L._make(len(at), k, n, 3, 20, k)
+    x = torch.zeros(rows, k, dtype=torch.uint8, device="cuda")
+    x[at] = sx.contiguous().view(torch.uint8)
+    xs = torch.ones(rows, device="cuda")
+    xs[at] = sxs
+    of_row = torch.full((rows,), 1, dtype=torch.int32, device="cuda")
+    of_row[at] = of
+    y = O.linear8(x.view(O.F8), xs, w, ws, bias, ad, of_row)
+    L._check(y[at], (sx, sxs, w, ws, bias, ad, of))
+    rest = torch.arange(5, rows, 9973, device="cuda")
+    rest = rest[~torch.isin(rest, at)]
+    assert torch.equal(y[rest], bias.bfloat16().expand(len(rest), n))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows, cols", [(530_000, 4096), (60_000, 36_000)])
+def test_norm_past_2_31_elements(rows, cols):
+    """Rows that stay in registers and rows that are read again."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    assert rows * cols > 2 ** 31
+    at = torch.tensor([0, 1, rows // 2, rows - 2, rows - 1], device="cuda")
+    torch.manual_seed(cols)
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    r = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[at] = torch.randn(len(at), cols, device="cuda").bfloat16()
+    h, y, scale = O.add_rms_norm(x, None, r)
+    small = O.add_rms_norm(x[at], None, r[at])
+    assert torch.equal(h[at], small[0]) and torch.equal(y[at].view(torch.uint8), small[1].view(torch.uint8))
+    assert torch.equal(scale[at], small[2])
+    rest = torch.arange(7, rows - 7, 997, device="cuda")
+    rest = rest[~torch.isin(rest, at)]
+    assert (h[rest] == 2).all() and (y[rest].float() == 448).all()
