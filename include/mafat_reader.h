@@ -2,7 +2,7 @@
  * mafat_reader.h -- C ABI of the operators of a reader: a decoder whose
  * tokens, of many requests at once, read the feature maps that a plan's
  * network (mafat.h) leaves on the device.  They are not part of the paper's
- * method; they consume its output where it lies.
+ * method; they consume its output where it lies.  Forward only.
  *
  *   mafat_add_rms_norm     residual addition and root-mean-square norm, into
  *                          float32, bfloat16 or 8 bits with a scale per row
@@ -81,8 +81,10 @@ typedef struct {
  *   adapters a host struct, read during the call, or NULL
  *   workspace  mafat_linear_workspace bytes, 256-byte aligned (NULL if 0)
  * Sums are float32.  The 8-bit matrix instructions align the products of a
- * step before they add them: a sum is within about 2e-5 of the exact one,
- * relative to the root of the sum of its squared products.  Errors: EINVAL
+ * step before they add them: a sum is 1.5e-5 from the exact one on average and
+ * below 1e-4 singly, relative to the root of the sum of its squared products.
+ * in_cols, strides and addresses of x and w in whole 16 bytes run an order of
+ * magnitude faster than others where rows are many.  Errors: EINVAL
  * (null or misaligned pointer, negative size, in_cols or out_cols < 1,
  * stride below the row length, bad adapters, y overlapping an input),
  * EWORKSPACE, EUNSUPPORTED (rank > 128, sizes or a stride of 2^22 or more

@@ -31,7 +31,10 @@ namespace {
 // positions of its split, 64 at a time through LDS: waves 0 and 1 (rows 0-31
 // and 32-63) take the first 32 of them and waves 2 and 3 the others, and the
 // two are joined at the end.  DP: head_dim rounded up; the values past it are
-// zeros in LDS.
+// zeros in LDS.  Bound by its loads, which go through registers and, unaligned,
+// in small pieces: 4096 rows, 5776 positions and 16 heads of 127 take 1.40 ms
+// (of 128, on cross_tile_kernel, 0.20), 64 rows of 8 frames of 1444 and 32/8 heads
+// of 127 55 us (of 128 18).
 constexpr int kRowTile = 64, kKeyTile = 64;
 
 template <int DT, int DP>

@@ -69,8 +69,12 @@ __device__ __forceinline__ unsigned lds_offset(const void* p) {
   return static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_ptr_t)p));
 }
 
-constexpr float kLazy = 8.f;  // the running maximum may lag by a factor of 2^8 of the sums before they are rescaled
-
+// The running maximum may lag by a factor of 2^8 of the sums before they are
+// rescaled, all rows of a wave together (rescaling a softmax's sums only past a
+// threshold is published; float32 has room for the factor, and the bfloat16
+// exponentials keep their relative accuracy).  A row's last bits so depend on
+// its wave's other rows.
+constexpr float kLazy = 8.f;
 
 // Bytes of a mask as bits.  A lane holds those of 64 positions, so a wave looks
 // 4096 ahead with four loads a lane.
@@ -385,9 +389,14 @@ struct Fetch {
 // Per 64 keys a wave spends 1024 cycles in matrix instructions (DP 128) and
 // about as many on the vector ALUs, a third of them in the exponentials; its LDS
 // reads take 128.  The largest score lags (kLazy), so the sums are seldom
-// rescaled.  2 frames x 2048 rows x 16 heads of 128, 5776 positions: 197 us,
-// 985 TFLOP/s, where a large bfloat16 product of the library reaches 1590; matrix
-// instructions are busy 38 % of the time, at a clock that both bring down to 2.0 GHz.
+// rescaled.  2 frames x 2048 rows x 16 heads of 128, 5776 positions: 195 us,
+// 994 TFLOP/s, where a large bfloat16 product of the library reaches 1590; matrix
+// instructions are busy 39 % of the time, at a clock that both bring down to 2.1 GHz.
+// Scores, softmax and outputs of a tile follow each other in every wave, and a
+// barrier a tile keeps the waves of a SIMD together, so the two kinds of work
+// seldom overlap.  With a mask by key 212 us; by row 443 (a lane reads its own
+// mask, and registers spill from heads of 96 on); heads of 256 with a mask by
+// row spill 285 registers: 4.9 ms, where without a mask they take 0.59.
 template <int DT, int DP, int MASK, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs a) {
   using F = Fast<DT, DP>;
@@ -470,8 +479,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs 
 // another before the end, where the parts are joined in LDS.  The slots of a
 // block take at most 67 KB, so that two blocks share a CU: their waves fetch
 // while others compute, and a ragged call's blocks run in one round (8 frames,
-// 64 rows, 8 heads of 128, up to 1444 positions: 11.7 us and
-// 3.9 for the join; 4 rows, 64980 positions, 4 heads of 128 for 16: 97 us, 5.5 TB/s,
+// 64 rows, 8 heads of 128, up to 1444 positions: 11.6 us and
+// 4.0 for the join; 4 rows, 64980 positions, 4 heads of 128 for 16: 97 us, 5.5 TB/s,
 // the rate of a copy).
 template <int DT, int DP, int MASK>
 __global__ __launch_bounds__(64 * cross_few_waves(DT, DP), 1) void cross_few_kernel(const CrossArgs a) {
