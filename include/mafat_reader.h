@@ -140,7 +140,7 @@ typedef struct {
  * the second product as the sum of two bfloat16 parts (16 bits) where a frame
  * has up to 64 pairs of a row and a head that share a key/value head (rows /
  * frames counted alike), or where head_dim, or an address or stride of k or v,
- * is no multiple of 16 bytes; else rounded to bfloat16, each by its own size.
+ * is no multiple of 16 bytes, or scale is 0; else rounded to bfloat16, each by its own size.
  * So, and because rows of a wave rescale their sums together, the last bits of
  * a row may depend on the rows that share its call.  Errors: EINVAL
  * (null or misaligned pointer, bad size or stride, rows not divisible without

@@ -335,15 +335,17 @@ void launch_any(const CrossArgs& a, dim3 grid, hipStream_t stream) {
   else hipLaunchKernelGGL((cross_any_kernel<DT, DP, MASK_ROWS>), grid, dim3(256), 0, stream, a);
 }
 
-// Whole 16-byte pieces, offsets of a tile's 64 rows in 31 bits, and heads whose
-// sums fit the registers.
+// Whole 16-byte pieces, offsets of a tile's 64 rows in 31 bits, heads whose
+// sums fit the registers, and a scale other than zero (which cross_fast.h
+// divides by; cross_any_kernel takes products that are not finite to NaN by it).
 template <int DT>
 bool fast(const CrossArgs& a) {
   constexpr int64_t esz = sizeof(typename Elt<DT>::T);
   const auto whole = [](const void* p, int64_t x, int64_t y, int64_t z) {
     return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(esz * (x | y | z))) & 15) == 0;
   };
-  return a.head_dim * esz % 16 == 0 && (DT == MAFAT_BF16 || a.head_dim <= 128) && a.k_pos < (1 << 22) && a.v_pos < (1 << 22) &&
+  return a.scale != 0.f && a.head_dim * esz % 16 == 0 && (DT == MAFAT_BF16 || a.head_dim <= 128) &&
+         a.k_pos < (1 << 22) && a.v_pos < (1 << 22) &&
          whole(a.k, a.k_frame, a.k_pos, a.k_head) && whole(a.v, a.v_frame, a.v_pos, a.v_head);
 }
 

@@ -141,10 +141,10 @@ struct Rows {
     row = at.row0 + in_frame;
     head = kv * a.group + rr - in_frame * a.group;
     // A negative scale goes into the rows' sign, so that the largest product has
-    // the largest score; a scale of zero makes them zero (minus infinity stands
-    // for masked keys and must not meet it).
-    const uint32_t flip = a.scale < 0.f ? (DT == MAFAT_BF16 ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale == 0.f ? 0u : ~0u;
-    scale = a.scale == 0.f ? 1.f : fabsf(a.scale);
+    // the largest score.  (A scale of zero is not for this kernel: minus infinity
+    // stands for masked keys and must not meet it.)
+    const uint32_t flip = a.scale < 0.f ? (DT == MAFAT_BF16 ? 0x80008000u : 0x80000000u) : 0u;
+    scale = a.scale < 0.f ? -a.scale : a.scale;
     // Finite for any scale: plus infinity would make no product larger than a
     // maximum of minus infinity, and the first key would not be taken for one.
     lazy = fminf(kLazy / scale, 0x1.fffffep127f);
@@ -155,7 +155,7 @@ struct Rows {
       qf[t] = u32x4{0, 0, 0, 0};
       if (d < D) __builtin_memcpy(&qf[t], q + d, 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qf[t][i] = (qf[t][i] ^ flip) & keep;
+      for (int i = 0; i < 4; ++i) qf[t][i] ^= flip;
     }
     most = kNone;
     sum = 0.f;
@@ -396,7 +396,7 @@ struct Fetch {
 // barrier a tile keeps the waves of a SIMD together, so the two kinds of work
 // seldom overlap.  With a mask by key 212 us; by row 443 (a lane reads its own
 // mask, and registers spill from heads of 96 on); heads of 256 with a mask by
-// row spill 285 registers: 4.9 ms, where without a mask they take 0.59.
+// row spill 300 registers: 4.9 ms, where without a mask they take 0.59.
 template <int DT, int DP, int MASK, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void cross_tile_kernel(const CrossArgs a) {
   using F = Fast<DT, DP>;

@@ -56,3 +56,22 @@ def test_scores_past_float32(rows, s, d, dtype):
     # rows of a wave rescale their sums together, so the last bits may differ
     assert (y[others].float() - want[others].float()).abs().max() <= 2.0 ** -7
     assert (lse[others] - want_lse[others]).abs().max() <= 2.0 ** -18 * want_lse.abs().max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 33])
+@pytest.mark.parametrize("rows", [6, 200])
+def test_a_scale_of_zero_keeps_nan(rows, d, dtype):
+    """Zero times NaN or infinity; the other rows get the mean of the values."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    a = _make(1, rows, 150, 2, 1, d, dtype, 5)
+    want, want_lse = O.cross_attention(**a, scale=0.0, lse=True)
+    a["q"][1, 0, 5], a["q"][3, 1, 30] = float("nan"), float("-inf")
+    y, lse = O.cross_attention(**a, scale=0.0, lse=True)
+    bad = torch.zeros(rows, 2, dtype=torch.bool, device="cuda")
+    bad[1, 0] = bad[3, 1] = True
+    assert torch.isnan(y[bad]).all() and torch.isnan(lse[bad]).all()
+    assert torch.equal(y[~bad], want[~bad]) and torch.equal(lse[~bad], want_lse[~bad])
