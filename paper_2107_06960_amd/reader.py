@@ -65,7 +65,10 @@ class Reader:
 
     def run(self, tokens, y, q_offsets=None, row_adapter=None, k_lengths=None, key_mask=None):
         """tokens: bfloat16 [rows, width], as y has to be, frame by frame; q_offsets: int32 [frames + 1], the frames' rows (None: as many
-        each); row_adapter: int32 [rows], the adapter of each row's request.  Returns the normed rows."""
+        each); row_adapter: int32 [rows], the adapter of each row's request, for layers that have adapters (None: without
+        them).  Returns the normed rows."""
+        if row_adapter is not None and not any(p[i]["adapters"] for p in self.params["layers"] for i in ("q", "o")):
+            raise ValueError("row_adapter names adapters, but no layer has any")
         k, v = self.states(y)
         rows, h, delta = tokens.shape[0], tokens, None
 

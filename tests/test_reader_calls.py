@@ -28,3 +28,11 @@ def test_assembly_puts_m0_back():
 def test_a_scale_has_to_be_finite_in_base_2(scale, status):
     n = ctypes.c_size_t()
     assert O.lib().mafat_cross_workspace(ctypes.byref(O.mafat_cross(**dict(CROSS, scale=scale))), ctypes.byref(n)) == status
+
+
+def test_a_reader_without_adapters_refuses_the_rows_adapters():
+    import torch
+    from paper_2107_06960_amd import reader as R
+    reader = R.Reader(R.draw_params(64, 2, 32, 1, device="cpu"), 2, 1, 32)
+    with pytest.raises(ValueError, match="row_adapter"):
+        reader.run(torch.zeros(2, 64), torch.zeros(1, 2, 2, 64), row_adapter=torch.zeros(2, dtype=torch.int32))
