@@ -10,6 +10,11 @@
  *                          low-rank adapters of the requests beside it
  *   mafat_cross_attention  attention of the requests' tokens to the positions
  *                          of the frames they are about
+ *   mafat_rotary           positions of queries and keys as rotations
+ *   mafat_decay_attention  linear attention among the tokens of a request, with
+ *                          a decay for each head and a state that is kept
+ *   mafat_block_norm       norms after and before a block with its gate, its
+ *                          residual scale and the residual addition
  *
  * Conventions of mafat.h hold: device buffers are the caller's, run functions
  * enqueue kernels on the given stream and return, no device memory is
@@ -152,6 +157,123 @@ int mafat_cross_workspace(const mafat_cross* c, size_t* bytes);
 int mafat_cross_attention(const mafat_cross* c, const void* q, const void* k, const void* v,
                           const int32_t* q_offsets, const int32_t* k_lengths, const unsigned char* mask,
                           void* y, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* Sizes and strides of mafat_rotary.  y: where the turned values go. */
+typedef struct {
+  int32_t dtype;               /* MAFAT_F32 or MAFAT_BF16: q, k and their outputs */
+  int32_t axes;                /* numbers of a position: 1 .. 4 */
+  int64_t rows;
+  int32_t q_heads, k_heads;    /* k_heads 0: no k */
+  int32_t head_dim;            /* 1 .. 1024 */
+  int32_t pairs;               /* the first 2 * pairs values of a head turn */
+  int32_t interleaved;         /* pair i: 0: values i and pairs + i; 1: values 2 i and 2 i + 1 */
+  float magnitude;             /* of the turned values */
+  int64_t q_row, q_head, k_row, k_head;
+  int64_t qy_row, qy_head, ky_row, ky_head;
+} mafat_turns;
+
+/* For every row r, head and pair i, with t = sum_a positions[r][a] * turns[a][i]
+ * (in turns, so angles are 2 pi t):
+ *   (x1, x2) -> magnitude * (x1 cos - x2 sin, x2 cos + x1 sin)
+ * and the values of a head behind its pairs as they are.
+ *   positions  int32 [rows][axes], contiguous; negative ones turn back
+ *   turns      float64 [axes][pairs], contiguous: turns per step, for instance
+ *              base^(-i / pairs) / (2 pi)
+ *   qy, ky     may be q and k themselves (with their strides); otherwise outputs
+ *              may not overlap inputs or each other
+ * t is formed and brought below half a turn in float64, its sine and cosine in
+ * float32: far positions keep the accuracy of near ones.  Errors: EINVAL (null
+ * or misaligned pointer, negative rows or heads, axes outside 1 .. 4, pairs < 0
+ * or 2 * pairs > head_dim, stride below head_dim, magnitude not finite,
+ * overlap), EUNSUPPORTED (dtype, head_dim > 1024, rows of 2^31 or more, more
+ * than 65535 heads, strides of 2^31 or more), EHIP. */
+int mafat_rotary(const mafat_turns* c, const int32_t* positions, const double* turns, const void* q, const void* k,
+                 void* qy, void* ky, void* stream);
+
+/* Sizes and strides of mafat_block_norm.  After and before: of the block whose
+ * output is x, and of the next one. */
+typedef struct {
+  int32_t dtype;        /* MAFAT_F32 or MAFAT_BF16: x, gate, residual and sum */
+  int32_t out_dtype;    /* MAFAT_F32, MAFAT_BF16 or MAFAT_F8: y */
+  int64_t rows, cols;
+  int32_t after;        /* norm x, in `groups` equal parts of a row */
+  int32_t groups;       /* 1 .. 4096, divides cols */
+  int32_t gate_act;     /* of the gate: 0 sigmoid, 1 gate * sigmoid(gate) */
+  int32_t before;       /* norm the sum */
+  float eps;
+  int64_t x_stride, gate_stride, residual_stride, sum_stride, y_stride;
+} mafat_block;
+
+/* Per row:
+ *   u = x * (mean of its part (x^2) + eps)^(-1/2) * after_gain    if after
+ *   u = u * act(gate)                                             with a gate
+ *   h = residual + scale * u          (scale 1 and residual 0 without them)
+ *   y = h * (mean(h^2) + eps)^(-1/2) * before_gain                if before
+ * in float32 throughout: sum is h rounded to dtype, y follows from h before that
+ * rounding.  y and y_scale as in mafat_add_rms_norm.
+ *   x, gate, residual, sum   rows x cols in dtype; gate NULL: none; residual
+ *                            and sum go together, or are NULL
+ *   after_gain, scale, before_gain   float32[cols], or NULL (ones)
+ *   y, y_scale               rows x cols in out_dtype, float32[rows] for MAFAT_F8
+ * Outputs may not overlap inputs or each other.  Errors: EINVAL (null or
+ * misaligned pointer, negative rows, cols < 1, groups that do not divide cols, a
+ * gain without its norm, stride below cols, one of residual and sum without
+ * the other, a scale pointer that does not match out_dtype, overlap, eps
+ * negative or not finite), EUNSUPPORTED (dtype; rows, cols or a stride of 2^31 or
+ * more, groups > 4096), EHIP. */
+int mafat_block_norm(const mafat_block* c, const void* x, const float* after_gain, const void* gate, const float* scale,
+                     const void* residual, void* sum, const float* before_gain, void* y, float* y_scale, void* stream);
+
+/* Sizes and strides of mafat_decay_attention.  Rows are the tokens of all
+ * requests, request by request; every query head h reads the keys, values and
+ * states of head h / (q_heads / kv_heads). */
+typedef struct {
+  int32_t dtype;              /* MAFAT_F32 or MAFAT_BF16: q, k, v and y */
+  int32_t requests;
+  int64_t rows;               /* tokens of all requests together */
+  int64_t slots;              /* states in the pool */
+  int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
+  int32_t key_dim, value_dim; /* 1 .. 256 each */
+  float scale;
+  int32_t decay_by_row;       /* 0: log_decay [kv_heads]; 1: [rows][kv_heads] */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, y_row, y_head;
+  int64_t decay_row;          /* between rows of log_decay, if by row */
+  int64_t state_slot;         /* between states of the pool */
+} mafat_decay;
+
+/* For every request, its tokens t = 1, 2, ... in order, and every key/value head:
+ *   S_t = exp(log_decay_t) S_{t-1} + k_t v_t^T      (key_dim x value_dim)
+ *   y_t = scale * q_t S_t                           for the query heads of it
+ * where S_0 is the request's state in the pool, which ends up as the last S.
+ *   log_decay  float32; above 0 counts as 0, below -138 (a factor that float32
+ *              ends at) as -138; NaN makes what follows NaN
+ *   offsets    int32[requests + 1], not decreasing, each clamped to [0, rows]:
+ *              request i's rows are [offsets[i], offsets[i + 1]); rows that no
+ *              request has are not written, and requests without rows leave their
+ *              state.  (Offsets that decrease leave it open which rows are
+ *              computed.)  NULL: rows / requests each (rows must divide)
+ *   states     float32 [slots][kv_heads][key_dim][value_dim], the last three
+ *              contiguous, updated in place; NULL: every request starts from
+ *              zeros and nothing is kept
+ *   slots      int32[requests], each request's state; outside [0, slots): starts
+ *              from zeros and is not kept.  A state belongs to the first request
+ *              with rows that names it: later ones that name it too get y = NaN
+ *              and do not change it.  NULL: request i has state i
+ *   workspace  mafat_decay_workspace bytes, 256-byte aligned (NULL if 0)
+ * States and sums are float32.  Long requests are cut into segments whose states
+ * are joined, so the last bits of a row may depend on the sizes of the call.  What is
+ * not finite in a token reaches its own request's rows from that token on, and its
+ * state.  In bfloat16, scores and the states that rows read enter the matrix
+ * products in bfloat16 parts; the states that are kept do not lose by it.  Errors:
+ * EINVAL (null or misaligned pointer, bad size or stride, rows not divisible
+ * without offsets, scale not finite, an output overlapping another tensor),
+ * EWORKSPACE, EUNSUPPORTED (dtype, key_dim or value_dim > 256, rows * q_heads or
+ * requests * kv_heads of 2^31 or more, more than 65535 kv_heads, strides of 2^31
+ * bytes or more), EHIP. */
+int mafat_decay_workspace(const mafat_decay* c, size_t* bytes);
+int mafat_decay_attention(const mafat_decay* c, const void* q, const void* k, const void* v, const float* log_decay,
+                          const int32_t* offsets, float* states, const int32_t* slots, void* y, void* workspace,
+                          size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,361 @@
+// block_norm.hip -- the norm after a block, its gate, its residual scale, the
+// residual addition and the norm before the next block, into float32, bfloat16
+// or 8 bits with a scale per row.
+//
+//   u = x (mean_part x^2 + eps)^(-1/2) after_gain act(gate)
+//   h = residual + scale u,  y = h (mean h^2 + eps)^(-1/2) before_gain
+//
+// Bound by memory: x, gate and residual are read once, sum and y written once.
+// As in norm.hip a row stays in the registers of its team of threads; the
+// norm after takes a sum over each of the row's parts, the one before a sum over
+// the row, and 8 bits a maximum.
+#include <hip/hip_runtime.h>
+
+#include "norm_device.h"
+#include "reader.h"
+
+namespace mafat {
+namespace {
+
+__device__ __forceinline__ float gate_of(float g, int silu) { return (silu ? g : 1.f) / (1.f + expf(-g)); }
+
+// n of the V floats at p (the rest are zero).
+template <int V>
+__device__ __forceinline__ void load_gain(const float* p, int n, float (&g)[V]) {
+  if (n >= V) {
+    __builtin_memcpy(g, p, 4 * V);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = i < n ? p[i] : 0.f;
+  }
+}
+
+// How the sums of a row's parts are formed: the row is one part; a part is a
+// power of two of neighbouring lanes; parts of whole pieces, through LDS.
+enum { PARTS_ROW = 0, PARTS_LANES = 1, PARTS_LDS = 2 };
+
+// One row per team, NP pieces per thread at most.
+template <int DT, int OUT, int TEAM, int NP, int PARTS>
+__global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(const BlockArgs a) {
+  using T = typename Elt<DT>::T;
+  constexpr int V = Piece<DT>::V;
+  constexpr int TEAMS = TEAM >= 256 ? 1 : 256 / TEAM;
+  static_assert(TEAM <= 64 || TEAM >= 256, "a team is part of a wave, or the block");
+  static_assert(PARTS != PARTS_LDS || TEAM >= 256, "sums of parts in LDS are the block's");
+  __shared__ float lds_a[TEAM > 64 ? TEAM / 64 : 1], lds_b[TEAM > 64 ? TEAM / 64 : 1];
+  __shared__ uint32_t lds_max[TEAM > 64 ? TEAM / 64 : 1];
+  __shared__ float lds_part[PARTS == PARTS_LDS ? TEAM * NP : 1], lds_inv[PARTS == PARTS_LDS ? TEAM * NP : 1];
+  const int t = static_cast<int>(threadIdx.x) % TEAM;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * TEAMS + static_cast<int>(threadIdx.x) / TEAM;
+  if (row >= a.rows) return;  // whole teams; a team of several waves is the block
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+
+  float h[NP][V], g[NP][V], r[NP][V];
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const int c = (k * TEAM + t) * V;
+    load_piece<DT>(x + c, a.cols - c, h[k]);
+  }
+  if (a.gate) {
+    const T* gate = static_cast<const T*>(a.gate) + row * a.gate_stride;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const int c = (k * TEAM + t) * V;
+      load_piece<DT>(gate + c, a.cols - c, g[k]);
+    }
+  }
+  if (a.res) {
+    const T* res = static_cast<const T*>(a.res) + row * a.res_stride;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const int c = (k * TEAM + t) * V;
+      load_piece<DT>(res + c, a.cols - c, r[k]);
+    }
+  }
+  if (a.after) {
+    float inv[NP];
+    if constexpr (PARTS == PARTS_ROW) {
+      float sq = 0.f;
+#pragma unroll
+      for (int k = 0; k < NP; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sq = fmaf(h[k][i], h[k][i], sq);
+      sq = team_reduce<TEAM>(sq, Add{}, lds_a);
+      const float one = 1.f / sqrtf(sq / static_cast<float>(a.cols) + a.eps);
+#pragma unroll
+      for (int k = 0; k < NP; ++k) inv[k] = one;
+    } else {
+      const int pieces = a.part / V;  // of a part
+      float sq[NP];
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        sq[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sq[k] = fmaf(h[k][i], h[k][i], sq[k]);
+      }
+      if constexpr (PARTS == PARTS_LANES) {
+        for (int o = pieces >> 1; o > 0; o >>= 1)
+#pragma unroll
+          for (int k = 0; k < NP; ++k) sq[k] += __shfl_xor(sq[k], o, 64);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) inv[k] = 1.f / sqrtf(sq[k] / static_cast<float>(a.part) + a.eps);
+      } else {
+        const int lane = t & 63;
+#pragma unroll
+        for (int k = 0; k < NP; ++k) lds_part[k * TEAM + t] = sq[k];
+        __syncthreads();
+        for (int p = t >> 6; p < a.groups; p += TEAM / 64) {
+          float s = 0.f;
+          for (int i = lane; i < pieces; i += 64) s += lds_part[p * pieces + i];
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+          if (lane == 0) lds_inv[p] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NP; ++k) inv[k] = lds_inv[min((k * TEAM + t) / pieces, a.groups - 1)];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] *= inv[k];
+    if (a.after_gain) {
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        const int c = (k * TEAM + t) * V;
+        float w[V];
+        load_gain<V>(a.after_gain + c, a.cols - c, w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[k][i] *= w[i];
+      }
+    }
+  }
+  if (a.gate) {
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] *= gate_of(g[k][i], a.silu);
+  }
+  if (a.scale) {
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const int c = (k * TEAM + t) * V;
+      float w[V];
+      load_gain<V>(a.scale + c, a.cols - c, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] *= w[i];
+    }
+  }
+  if (a.res) {
+    T* sum = static_cast<T*>(a.sum) + row * a.sum_stride;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const int c = (k * TEAM + t) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] += r[k][i];
+      store_piece<DT>(sum + c, a.cols - c, h[k]);
+    }
+  }
+  if (a.before) {
+    float sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if ((k * TEAM + t) * V + i < a.cols) sq = fmaf(h[k][i], h[k][i], sq);
+    sq = team_reduce<TEAM>(sq, Add{}, lds_b);
+    const float inv = 1.f / sqrtf(sq / static_cast<float>(a.cols) + a.eps);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const int c = (k * TEAM + t) * V;
+      float w[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[i] = 1.f;
+      if (a.before_gain) load_gain<V>(a.before_gain + c, a.cols - c, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] *= inv * w[i];
+    }
+  }
+  using Y = typename OutElt<OUT>::T;
+  Y* y = static_cast<Y*>(a.y) + row * a.y_stride;
+  if constexpr (OUT == MAFAT_F8) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if ((k * TEAM + t) * V + i < a.cols) most = MaxBits{}(most, __float_as_uint(h[k][i]) & 0x7fffffffu);
+    most = team_reduce<TEAM>(most, MaxBits{}, lds_max);
+    float by;
+    const float scale = row_scale(most, &by);
+    if (t == 0) a.y_scale[row] = scale;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[k][i] *= by;
+  }
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const int c = (k * TEAM + t) * V;
+    store_piece<OUT>(y + c, a.cols - c, h[k]);
+  }
+}
+
+// Rows and parts of any length: a block of 1024 threads, value by value, reads
+// its row again for every step (from the caches, mostly).
+template <int DT, int OUT>
+__global__ __launch_bounds__(1024) void block_norm_any_kernel(const BlockArgs a) {
+  using T = typename Elt<DT>::T;
+  using Y = typename OutElt<OUT>::T;
+  constexpr int TEAM = 1024, WAVES = TEAM / 64;
+  __shared__ float lds_inv[4096];
+  __shared__ float lds_sum[2][WAVES];
+  __shared__ uint32_t lds_max[WAVES];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + row * a.gate_stride : nullptr;
+  const T* res = a.res ? static_cast<const T*>(a.res) + row * a.res_stride : nullptr;
+  Y* y = static_cast<Y*>(a.y) + row * a.y_stride;
+  if (a.after) {
+    if (a.groups == 1) {
+      float s = 0.f;
+      for (int64_t i = tid; i < a.cols; i += TEAM) s = fmaf(to_f(x[i]), to_f(x[i]), s);
+      s = team_reduce<TEAM>(s, Add{}, lds_sum[0]);
+      if (tid == 0) lds_inv[0] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+    } else {
+      for (int p = tid >> 6; p < a.groups; p += WAVES) {
+        float s = 0.f;
+        const T* at = x + static_cast<int64_t>(p) * a.part;
+        for (int i = lane; i < a.part; i += 64) s = fmaf(to_f(at[i]), to_f(at[i]), s);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+        if (lane == 0) lds_inv[p] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+      }
+    }
+    __syncthreads();
+  }
+  const auto sum_at = [&](int64_t c) {
+    float u = to_f(x[c]);
+    if (a.after) {
+      u *= lds_inv[static_cast<int>(c) / a.part];
+      if (a.after_gain) u *= a.after_gain[c];
+    }
+    if (gate) u *= gate_of(to_f(gate[c]), a.silu);
+    if (a.scale) u *= a.scale[c];
+    return res ? u + to_f(res[c]) : u;
+  };
+  float inv = 1.f;
+  if (a.before || res) {
+    T* sum = static_cast<T*>(a.sum) + row * a.sum_stride;
+    float s = 0.f;
+    for (int64_t c = tid; c < a.cols; c += TEAM) {
+      const float h = sum_at(c);
+      if (res) store1(sum + c, h);
+      s = fmaf(h, h, s);
+    }
+    if (a.before) inv = 1.f / sqrtf(team_reduce<TEAM>(s, Add{}, lds_sum[1]) / static_cast<float>(a.cols) + a.eps);
+  }
+  const auto out_at = [&](int64_t c) {
+    const float h = sum_at(c);
+    return a.before ? h * (a.before_gain ? inv * a.before_gain[c] : inv) : h;
+  };
+  float by = 1.f;
+  if constexpr (OUT == MAFAT_F8) {
+    uint32_t most = 0;
+    for (int64_t c = tid; c < a.cols; c += TEAM) most = MaxBits{}(most, __float_as_uint(out_at(c)) & 0x7fffffffu);
+    most = team_reduce<TEAM>(most, MaxBits{}, lds_max);
+    const float scale = row_scale(most, &by);
+    if (tid == 0) a.y_scale[row] = scale;
+  }
+  for (int64_t c = tid; c < a.cols; c += TEAM) {
+    if constexpr (OUT == MAFAT_F8) {
+      y[c] = static_cast<Y>(__builtin_amdgcn_cvt_pk_fp8_f32(out_at(c) * by, 0.f, 0, false) & 0xff);
+    } else {
+      store1(y + c, out_at(c));
+    }
+  }
+}
+
+// A launch has fewer than 2^32 threads: where a row per block would pass
+// that, `most` rows after another go in a launch of their own.
+template <int DT, int OUT, typename F>
+hipError_t by_rows(const BlockArgs& a, int64_t most, F launch_rows) {
+  using T = typename Elt<DT>::T;
+  using Y = typename OutElt<OUT>::T;
+  for (int64_t at = 0; at < a.rows; at += most) {
+    BlockArgs p = a;
+    p.rows = a.rows - at < most ? a.rows - at : most;
+    p.x = static_cast<const T*>(a.x) + at * a.x_stride;
+    if (a.gate) p.gate = static_cast<const T*>(a.gate) + at * a.gate_stride;
+    if (a.res) {
+      p.res = static_cast<const T*>(a.res) + at * a.res_stride;
+      p.sum = static_cast<T*>(a.sum) + at * a.sum_stride;
+    }
+    p.y = static_cast<Y*>(a.y) + at * a.y_stride;
+    if (a.y_scale) p.y_scale = a.y_scale + at;
+    launch_rows(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int DT, int OUT>
+hipError_t launch(const BlockArgs& a, hipStream_t stream) {
+  constexpr int V = Piece<DT>::V;
+  constexpr int64_t kThreads = int64_t{1} << 31;  // of a launch, at most
+  const int64_t pieces = (static_cast<int64_t>(a.cols) + V - 1) / V;
+  const int each = a.part / V;  // pieces of a part
+  const bool one = !a.after || a.groups == 1, whole = a.part % V == 0;
+  const bool lanes = whole && each <= 64 && (each & (each - 1)) == 0;
+#define MAFAT_BLOCK(team_, np_, parts_)                                                                      \
+  do {                                                                                                       \
+    constexpr int teams = (team_) >= 256 ? 1 : 256 / (team_), block = (team_) > 256 ? (team_) : 256;         \
+    return by_rows<DT, OUT>(a, teams * (kThreads / block), [&](const BlockArgs& p) {                         \
+      hipLaunchKernelGGL((block_norm_kernel<DT, OUT, team_, np_, parts_>),                                   \
+                         dim3(static_cast<unsigned>((p.rows + teams - 1) / teams)), dim3(block), 0, stream, p); \
+    });                                                                                                      \
+  } while (0)
+  if (one) {
+    if (pieces <= 16) MAFAT_BLOCK(16, 1, PARTS_ROW);
+    if (pieces <= 64) MAFAT_BLOCK(64, 1, PARTS_ROW);
+    if (pieces <= 128) MAFAT_BLOCK(64, 2, PARTS_ROW);
+    if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_ROW);
+    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_ROW);
+    if (pieces <= 1024) MAFAT_BLOCK(1024, 1, PARTS_ROW);
+    if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_ROW);
+  } else if (lanes) {
+    if (pieces <= 64) MAFAT_BLOCK(64, 1, PARTS_LANES);
+    if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_LANES);
+    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_LANES);
+    if (pieces <= 1024) MAFAT_BLOCK(1024, 1, PARTS_LANES);
+    if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_LANES);
+  } else if (whole) {
+    if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_LDS);
+    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_LDS);
+    if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_LDS);
+  }
+#undef MAFAT_BLOCK
+  return by_rows<DT, OUT>(a, kThreads / 1024, [&](const BlockArgs& p) {
+    hipLaunchKernelGGL((block_norm_any_kernel<DT, OUT>), dim3(static_cast<unsigned>(p.rows)), dim3(1024), 0, stream, p);
+  });
+}
+
+template <int DT>
+hipError_t launch_in(int out_dtype, const BlockArgs& a, hipStream_t stream) {
+  switch (out_dtype) {
+    case MAFAT_F32: return launch<DT, MAFAT_F32>(a, stream);
+    case MAFAT_BF16: return launch<DT, MAFAT_BF16>(a, stream);
+    default: return launch<DT, MAFAT_F8>(a, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(int dtype, int out_dtype, const BlockArgs& a, hipStream_t stream) {
+  return dtype == MAFAT_BF16 ? launch_in<MAFAT_BF16>(out_dtype, a, stream) : launch_in<MAFAT_F32>(out_dtype, a, stream);
+}
+
+}  // namespace mafat

@@ -1,0 +1,408 @@
+// decay.hip -- linear attention with a decay for each head: tokens of a request
+// in order, a state of key_dim x value_dim per request and key/value head.
+//
+//   S_t = a_t S_{t-1} + k_t v_t^T,  y_t = scale q_t S_t
+//
+// Single tokens run token after token (decay_step_kernel), bound by reading and
+// writing the states.  Prompts run in chunks of C tokens, with c_i the sum of log a
+// over the chunk's tokens up to i:
+//   y_i = scale (e^{c_i} q_i S_0 + sum_{j <= i} e^{c_i - c_j} (q_i . k_j) v_j)
+//   S_C = e^{c_C} S_0 + sum_j e^{c_C - c_j} k_j v_j^T
+// all of it products of matrices; exponents are differences of later and earlier
+// sums, so none is above 0.  A block takes the chunks of one request and head in
+// turn, its part of the state in the registers of the matrix accumulators.
+// Where that leaves too few blocks, requests are cut into segments: a first launch
+// forms what each segment adds to the state, a second one turns these into the
+// states that the segments start from, the last one gives the outputs.
+#include "decay_device.h"
+
+namespace mafat {
+namespace {
+
+// ------------------------------------------------------------ single tokens
+
+// 64 columns of a state a block; a thread holds 4 of them in RPT of its rows.
+template <int DT, int RPT>
+__global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
+  using T = typename Elt<DT>::T;
+  __shared__ f32x4 part[4][16];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int id = a.first_block + static_cast<int>(blockIdx.x);
+  const int rh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.slices));
+  const int slice = id - rh * a.slices;
+  const int request = static_cast<int>(static_cast<uint32_t>(rh) / static_cast<uint32_t>(a.kv_heads));
+  const int kv = rh - request * a.kv_heads;
+  int first, n;
+  rows_of(a, request, &first, &n);
+  if (n == 0) return;
+  const int64_t slot = slot_of(a, request);
+  const int c = 64 * slice + 4 * (tid & 15), nc = a.value_dim - c, r0 = tid >> 4;
+  float* state = nullptr;
+  f32x4 s[RPT];
+  if (slot >= 0) {
+    state = a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim + c;
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const int r = r0 + 16 * i;
+      s[i] = load4<float>(state + static_cast<int64_t>(r) * a.value_dim, r < a.key_dim ? nc : 0);
+    }
+  } else {
+    const float f = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) s[i] = f32x4{f, f, f, f};
+  }
+  for (int t = 0; t < n; ++t) {
+    const int64_t row = first + t;
+    const T* kp = static_cast<const T*>(a.k) + row * a.k_row + kv * a.k_head;
+    const f32x4 v = load4<T>(static_cast<const T*>(a.v) + row * a.v_row + kv * a.v_head + c, nc);
+    const float g = __builtin_amdgcn_exp2f(decay_log2(a.log_decay[(a.decay_by_row ? row * a.decay_row : 0) + kv]));
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const int r = r0 + 16 * i;
+      const float k = r < a.key_dim ? to_f(kp[r]) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i][j] = fmaf(k, v[j], g * s[i][j]);
+    }
+    for (int h = 0; h < a.group; ++h) {
+      const int head = kv * a.group + h;
+      const T* qp = static_cast<const T*>(a.q) + row * a.q_row + head * a.q_head;
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const int r = r0 + 16 * i;
+        if (r < a.key_dim) {
+          const float q = to_f(qp[r]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = fmaf(q, s[i][j], y[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        y[j] += __shfl_xor(y[j], 16, 64);
+        y[j] += __shfl_xor(y[j], 32, 64);
+      }
+      if (lane < 16) part[wave][lane] = y;
+      __syncthreads();
+      if (tid < 16)
+        put4<T>(static_cast<T*>(a.y) + row * a.y_row + head * a.y_head + c, nc,
+                ((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid])) * a.scale);
+      __syncthreads();
+    }
+  }
+  if (state) {
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const int r = r0 + 16 * i;
+      if (r < a.key_dim) put4<float>(state + static_cast<int64_t>(r) * a.value_dim, nc, s[i]);
+    }
+  }
+}
+
+// ------------------------------------------------------------ prompts, any size
+
+// What a launch of the chunked kernels does: what a segment adds to the state,
+// or the outputs (and the last state).
+enum { ADDS = 0, OUTPUTS = 1 };
+
+// Any size, stride, alignment and type: 32 tokens at a time as float32 in LDS
+// and on the float32 matrix instructions (bfloat16 values are exact there).  A
+// block has 64 columns of the state, a wave 16 of them in KT tiles of 16 rows.
+// The 16x16x4 instruction's operands hold, in lane l, row (column) l % 16 and
+// the summed axis' entry l / 16; its result column l % 16 and rows 4 (l / 16) + r.
+// So the state's tile T is the operand of q S as it stands, if step r of the
+// instruction sums over the keys' entries 16 T + 4 (l / 16) + r.
+template <int DT, int KT, int MODE>
+__global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
+  using T = typename Elt<DT>::T;
+  constexpr int C = 32, KP = 16 * KT + 4, VP = 68, PP = 36;  // tokens; floats of a row of LDS
+  __shared__ __align__(16) float sk[C * KP];
+  __shared__ __align__(16) float sq[MODE == OUTPUTS ? C * KP : 4];
+  __shared__ __align__(16) float sv[C * VP];
+  __shared__ __align__(16) float sp[MODE == OUTPUTS ? C * PP : 4];
+  __shared__ double sc[C];
+  __shared__ int odd;  // whether the chunk's values are not all finite
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int l16 = lane & 15, h4 = lane >> 4;
+  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.blocks);
+  const int bh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.slices));
+  const int slice = id - bh * a.slices;
+  const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
+  const int kv = bh - b * a.kv_heads;
+  const Segment seg = find_segment(a, b);
+  if (!seg.any || (MODE == ADDS && seg.index + 1 == seg.count)) return;
+  const int c0 = 64 * slice, col = c0 + 16 * wave + l16;  // of the state
+  const int64_t slot = MODE == OUTPUTS && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
+  float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
+  float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
+
+  f32x4 s[KT];
+  if (MODE == OUTPUTS && (kept || seg.count > 1)) {
+    const float* from = seg.count > 1 ? part : kept;
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * i + 4 * h4 + r;
+        s[i][r] = row < a.key_dim && col < a.value_dim ? from[static_cast<int64_t>(row) * a.value_dim + col] : 0.f;
+      }
+  } else {
+    const float f = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) s[i] = f32x4{f, f, f, f};
+  }
+  double total = 0.0;
+  for (int t0 = 0; t0 < seg.n; t0 += C) {
+    const int n = min(C, seg.n - t0);
+    const int64_t row0 = seg.first + t0;
+    __syncthreads();
+    if (tid == 0) odd = 0;
+    __syncthreads();
+    for (int e = tid; e < C * 4 * KT; e += 256) {
+      const int r = e / (4 * KT), d = 4 * (e % (4 * KT));
+      const T* p = static_cast<const T*>(a.k) + (row0 + r) * a.k_row + kv * a.k_head + d;
+      *reinterpret_cast<f32x4*>(&sk[r * KP + d]) = load4<T>(p, r < n ? a.key_dim - d : 0);
+    }
+    for (int e = tid; e < C * 16; e += 256) {
+      const int r = e >> 4, d = 4 * (e & 15);
+      const T* p = static_cast<const T*>(a.v) + (row0 + r) * a.v_row + kv * a.v_head + c0 + d;
+      const f32x4 v = load4<T>(p, r < n ? a.value_dim - c0 - d : 0);
+      const float z = (v[0] - v[0]) + (v[1] - v[1]) + (v[2] - v[2]) + (v[3] - v[3]);
+      if (!(z == 0.f)) odd = 1;
+      *reinterpret_cast<f32x4*>(&sv[r * VP + d]) = v;
+    }
+    if (wave == 0) {
+      double g = 0.0;
+      if (lane < n) g = decay_log2(a.log_decay[(a.decay_by_row ? (row0 + lane) * a.decay_row : 0) + kv]);
+#pragma unroll
+      for (int o = 1; o < C; o <<= 1) {
+        const double left = __shfl_up(g, o, 64);
+        g += lane >= o ? left : 0.0;
+      }
+      if (lane < C) sc[lane] = g;
+    }
+    __syncthreads();
+    if constexpr (MODE == OUTPUTS) {
+      for (int h = 0; h < a.group; ++h) {
+        const int head = kv * a.group + h;
+        for (int e = tid; e < C * 4 * KT; e += 256) {
+          const int r = e / (4 * KT), d = 4 * (e % (4 * KT));
+          const T* p = static_cast<const T*>(a.q) + (row0 + r) * a.q_row + head * a.q_head + d;
+          *reinterpret_cast<f32x4*>(&sq[r * KP + d]) = load4<T>(p, r < n ? a.key_dim - d : 0);
+        }
+        __syncthreads();
+        {  // scores: a tile of 16 x 16 per wave, none above the diagonal
+          const int ti = wave >> 1, tj = wave & 1;
+          f32x4 p = {0.f, 0.f, 0.f, 0.f};
+          if (tj <= ti) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(&sq[(16 * ti + l16) * KP + 16 * i + 4 * h4]);
+              const f32x4 y = *reinterpret_cast<const f32x4*>(&sk[(16 * tj + l16) * KP + 16 * i + 4 * h4]);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], y[r], p, 0, 0, 0);
+            }
+          }
+          const int j = 16 * tj + l16;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = 16 * ti + 4 * h4 + r;
+            const float w = __builtin_amdgcn_exp2f(static_cast<float>(sc[i] - sc[j]));
+            sp[i * PP + j] = j <= i ? p[r] * w : 0.f;
+          }
+        }
+        f32x4 o[2];
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) {
+          o[ti] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < KT; ++i) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&sq[(16 * ti + l16) * KP + 16 * i + 4 * h4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], s[i][r], o[ti], 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[ti][r] *= __builtin_amdgcn_exp2f(static_cast<float>(sc[16 * ti + 4 * h4 + r]));
+        }
+        __syncthreads();
+        if (odd) {  // a later token's value must not reach a row, not even times zero
+#pragma unroll
+          for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int i = 16 * ti + 4 * h4 + r;
+              for (int j = 0; j <= i; ++j) o[ti][r] = fmaf(sp[i * PP + j], sv[j * VP + 16 * wave + l16], o[ti][r]);
+            }
+        } else {
+#pragma unroll
+          for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+            for (int tj = 0; tj <= ti; ++tj) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(&sp[(16 * ti + l16) * PP + 16 * tj + 4 * h4]);
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                o[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], sv[(16 * tj + 4 * h4 + r) * VP + 16 * wave + l16], o[ti], 0, 0, 0);
+            }
+        }
+        if (col < a.value_dim) {
+#pragma unroll
+          for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int i = 16 * ti + 4 * h4 + r;
+              if (i < n) store1(static_cast<T*>(a.y) + (row0 + i) * a.y_row + head * a.y_head + col, o[ti][r] * a.scale);
+            }
+        }
+        __syncthreads();
+      }
+    }
+    // the state after the chunk
+    total += sc[C - 1];
+    const float down = __builtin_amdgcn_exp2f(static_cast<float>(sc[C - 1]));
+#pragma unroll
+    for (int i = 0; i < KT; ++i) s[i] *= down;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = 16 * t + 4 * h4 + r;
+        const float v = sv[j * VP + 16 * wave + l16] * __builtin_amdgcn_exp2f(static_cast<float>(sc[C - 1] - sc[j]));
+#pragma unroll
+        for (int i = 0; i < KT; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(sk[j * KP + 16 * i + l16], v, s[i], 0, 0, 0);
+      }
+  }
+  float* const to = MODE == ADDS ? part : seg.index + 1 == seg.count ? kept : nullptr;
+  if (to) {
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * i + 4 * h4 + r;
+        if (row < a.key_dim && col < a.value_dim) to[static_cast<int64_t>(row) * a.value_dim + col] = s[i][r];
+      }
+  }
+  if (MODE == ADDS && slice == 0 && tid == 0)
+    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
+}
+
+// What segments add -> what they start from, for requests of several segments.
+// A thread takes one entry of a head's state through the segments.
+constexpr int kJoinAhead = 8;
+__global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
+  const int64_t size = static_cast<int64_t>(a.key_dim) * a.value_dim;
+  const int per = static_cast<int>((size + 255) / 256);
+  const int id = a.first_block + static_cast<int>(blockIdx.x);
+  const int rh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(per));
+  const int64_t e = static_cast<int64_t>(id - rh * per) * 256 + threadIdx.x;
+  const int request = static_cast<int>(static_cast<uint32_t>(rh) / static_cast<uint32_t>(a.kv_heads));
+  const int kv = rh - request * a.kv_heads;
+  // the request's first segment, and how many there are
+  const uint32_t len = static_cast<uint32_t>(a.segment);
+  int first, n;
+  rows_of(a, request, &first, &n);
+  const int count = static_cast<int>((static_cast<uint32_t>(n) + len - 1) / len);
+  if (count < 2) return;
+  uint32_t b = static_cast<uint32_t>(request) * static_cast<uint32_t>(count);
+  if (a.offsets) {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    b = 0;
+    for (int r = lane; r < request; r += 64) {
+      int lo, m;
+      rows_of(a, r, &lo, &m);
+      b += (static_cast<uint32_t>(m) + len - 1) / len;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) b += static_cast<uint32_t>(__shfl_xor(static_cast<int>(b), o, 64));
+  }
+  if (b + static_cast<uint32_t>(count) > static_cast<uint32_t>(a.segments)) return;  // (offsets that decrease)
+  const int64_t slot = slot_of(a, request);
+  if (e >= size) return;
+  float s = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
+  if (slot >= 0) s = a.states[slot * a.state_slot + kv * size + e];
+  float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * size + e;
+  const float* const factor = a.factor + static_cast<int64_t>(b) * a.kv_heads + kv;
+  const int64_t step = a.kv_heads * size;
+  for (int i0 = 0; i0 < count; i0 += kJoinAhead) {
+    float adds[kJoinAhead], by[kJoinAhead];
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i) {
+      const bool there = i0 + i + 1 < count;  // (the last adds nothing to another's start)
+      adds[i] = there ? part[(i0 + i) * step] : 0.f;
+      by[i] = there ? factor[static_cast<int64_t>(i0 + i) * a.kv_heads] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i) {
+      if (i0 + i < count) part[(i0 + i) * step] = s;
+      s = fmaf(s, by[i], adds[i]);
+    }
+  }
+}
+
+template <int DT, int MODE>
+hipError_t launch_any(DecayArgs a, hipStream_t stream) {
+  a.slices = (a.value_dim + 63) / 64;
+  const int64_t blocks = static_cast<int64_t>(a.segments) * a.kv_heads * a.slices;
+  if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
+  a.blocks = static_cast<int32_t>(blocks);
+  return for_block_parts(blocks, [&](int32_t from, unsigned n) {
+    a.first_block = from;
+    if (a.key_dim <= 64) hipLaunchKernelGGL((decay_any_kernel<DT, 4, MODE>), dim3(n), dim3(256), 0, stream, a);
+    else if (a.key_dim <= 128) hipLaunchKernelGGL((decay_any_kernel<DT, 8, MODE>), dim3(n), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((decay_any_kernel<DT, 16, MODE>), dim3(n), dim3(256), 0, stream, a);
+  });
+}
+
+hipError_t launch_join(DecayArgs a, hipStream_t stream) {
+  const int64_t blocks = static_cast<int64_t>(a.requests) * a.kv_heads * ((static_cast<int64_t>(a.key_dim) * a.value_dim + 255) / 256);
+  if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
+  return for_block_parts(blocks, [&](int32_t from, unsigned n) {
+    a.first_block = from;
+    hipLaunchKernelGGL(decay_join_kernel, dim3(n), dim3(256), 0, stream, a);
+  });
+}
+
+template <int DT>
+hipError_t launch_step(DecayArgs a, hipStream_t stream) {
+  a.slices = (a.value_dim + 63) / 64;
+  const int64_t blocks = static_cast<int64_t>(a.requests) * a.kv_heads * a.slices;
+  if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
+  return for_block_parts(blocks, [&](int32_t from, unsigned n) {
+    a.first_block = from;
+    if (a.key_dim <= 64) hipLaunchKernelGGL((decay_step_kernel<DT, 4>), dim3(n), dim3(256), 0, stream, a);
+    else if (a.key_dim <= 128) hipLaunchKernelGGL((decay_step_kernel<DT, 8>), dim3(n), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((decay_step_kernel<DT, 16>), dim3(n), dim3(256), 0, stream, a);
+  });
+}
+
+template <int DT>
+hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
+  if (p.recurrent) return launch_step<DT>(a, stream);
+  // (without offsets the requests' lengths are known)
+  if (p.split && (a.offsets || a.per_request > a.segment)) {
+    hipError_t e = launch_any<DT, ADDS>(a, stream);
+    if (e == hipSuccess) e = launch_join(a, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_any<DT, OUTPUTS>(a, stream);
+}
+
+}  // namespace
+
+DecayPlan plan_decay(const mafat_decay& c) {
+  DecayPlan p{};
+  // One or two tokens a request, if they are alike: a chunk would be nearly empty.
+  p.recurrent = c.rows <= 2 * int64_t{c.requests};
+  // Segments that leave about two blocks a CU, of 256 tokens at least.
+  const int64_t slices = (c.value_dim + 63) / 64;
+  int64_t len = (c.rows * c.kv_heads * slices + 511) / 512;
+  len = len < 256 ? 256 : (len + 63) / 64 * 64;
+  p.segment = len;
+  p.segments = c.rows / len + c.requests;
+  p.split = !p.recurrent && c.rows > len;
+  return p;
+}
+
+hipError_t launch_decay(int dtype, const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
+  return dtype == MAFAT_BF16 ? launch<MAFAT_BF16>(a, p, stream) : launch<MAFAT_F32>(a, p, stream);
+}
+
+}  // namespace mafat

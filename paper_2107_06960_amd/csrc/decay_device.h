@@ -1,0 +1,141 @@
+// decay_device.h -- device helpers that the kernels of linear attention with
+// decays share (decay.hip, decay_bf16.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_util.h"
+#include "reader.h"
+
+namespace mafat {
+namespace {
+
+constexpr double kLog2e = 1.4426950408889634;
+
+// A decay's logarithm in base 2, at most 0 and at least -200 (2^-200 is zero in
+// float32); NaN stays.
+__device__ __forceinline__ float decay_log2(float log_decay) {
+  const float l = log_decay > 0.f ? 0.f : log_decay < -138.f ? -138.6f : log_decay;
+  return static_cast<float>(static_cast<double>(l) * kLog2e);
+}
+
+// Rows of request i: first and number.
+__device__ __forceinline__ void rows_of(const DecayArgs& a, int i, int* first, int* n) {
+  if (!a.offsets) {
+    *first = i * a.per_request;
+    *n = a.per_request;
+    return;
+  }
+  *first = min(max(a.offsets[i], 0), a.rows);
+  *n = max(min(max(a.offsets[i + 1], 0), a.rows) - *first, 0);
+}
+
+// The state of a request's slot: NONE: starts from zeros and is not kept;
+// TAKEN: an earlier request with rows has it.  The same in all lanes.
+enum { SLOT_NONE = -1, SLOT_TAKEN = -2 };
+__device__ __forceinline__ int64_t slot_of(const DecayArgs& a, int request) {
+  if (!a.states) return SLOT_NONE;
+  const int s = a.slots ? a.slots[request] : request;
+  if (s < 0 || s >= a.pool) return SLOT_NONE;
+  if (a.slots) {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    for (int e0 = 0; e0 < request; e0 += 64) {
+      const int e = e0 + lane;
+      bool same = false;
+      if (e < request && a.slots[e] == s) {
+        int first, n;
+        rows_of(a, e, &first, &n);
+        same = n > 0;
+      }
+      if (__builtin_amdgcn_ballot_w64(same)) return SLOT_TAKEN;
+    }
+  }
+  return s;
+}
+
+// A block's work: a segment of a request.
+struct Segment {
+  int request, first, n;  // rows of the segment
+  int index, count;       // of the request's segments
+  bool any;
+};
+
+// Segment b of all requests together.  With offsets each wave scans the
+// requests, 64 at a time.
+__device__ __forceinline__ Segment find_segment(const DecayArgs& a, int b) {
+  Segment s;
+  s.any = true;
+  const uint32_t len = static_cast<uint32_t>(a.segment);
+  int start, rows;
+  if (!a.offsets) {
+    rows = a.per_request;
+    s.count = static_cast<int>((static_cast<uint32_t>(rows) + len - 1) / len);
+    s.request = static_cast<int>(static_cast<uint32_t>(b) / static_cast<uint32_t>(s.count));
+    s.index = b - s.request * s.count;
+    start = s.request * rows;
+    s.any = s.request < a.requests;
+  } else {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    uint32_t before = 0;
+    s.any = false;
+    s.request = s.index = s.count = start = rows = 0;
+    for (int r0 = 0; r0 < a.requests; r0 += 64) {
+      const int r = r0 + lane;
+      int lo = 0, n = 0;
+      if (r < a.requests) rows_of(a, r, &lo, &n);
+      const uint32_t blocks = (static_cast<uint32_t>(n) + len - 1) / len;
+      // (offsets that decrease may make the sums wrap: b then matches some request or none)
+      uint32_t upto = blocks;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t left = static_cast<uint32_t>(__shfl_up(static_cast<int>(upto), o, 64));
+        upto += lane >= o ? left : 0;
+      }
+      const uint32_t from = before + upto - blocks, mine = static_cast<uint32_t>(b) - from;
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(mine < blocks);
+      if (hit) {
+        const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+        s.request = r0 + l;
+        start = __builtin_amdgcn_readlane(lo, l);
+        rows = __builtin_amdgcn_readlane(n, l);
+        s.index = __builtin_amdgcn_readlane(static_cast<int>(mine), l);
+        s.count = __builtin_amdgcn_readlane(static_cast<int>(blocks), l);
+        s.any = true;
+        break;
+      }
+      before += static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(upto), 63));
+    }
+  }
+  s.first = start + s.index * a.segment;
+  s.n = min(a.segment, rows - s.index * a.segment);
+  return s;
+}
+
+// n of the 4 values at p as floats (the rest are zero).
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const T* p, int n) {
+  T t[4];
+  if (n >= 4) {
+    __builtin_memcpy(t, p, sizeof(t));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = i < n ? p[i] : static_cast<T>(0);
+  }
+  return f32x4{to_f(t[0]), to_f(t[1]), to_f(t[2]), to_f(t[3])};
+}
+template <typename T>
+__device__ __forceinline__ void put4(T* p, int n, f32x4 v) {
+  if (n >= 4) {
+    T t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store1(&t[i], v[i]);
+    __builtin_memcpy(p, t, sizeof(t));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) store1(p + i, v[i]);
+  }
+}
+
+}  // namespace
+}  // namespace mafat

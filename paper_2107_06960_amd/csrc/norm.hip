@@ -15,96 +15,11 @@
 // and the last one, if it is short, value by value.
 #include <hip/hip_runtime.h>
 
-#include "device_util.h"
+#include "norm_device.h"
 #include "reader.h"
 
 namespace mafat {
 namespace {
-
-template <int DT> struct Piece { static constexpr int V = 16 / sizeof(typename Elt<DT>::T); };
-
-// The V values of a piece that starts at p, `n` of which are there (the rest are zero).
-template <int DT>
-__device__ __forceinline__ void load_piece(const typename Elt<DT>::T* p, int n, float (&v)[Piece<DT>::V]) {
-  constexpr int V = Piece<DT>::V;
-  typename Elt<DT>::T t[V];
-  if (n >= V) {
-    __builtin_memcpy(t, p, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) t[i] = i < n ? p[i] : static_cast<typename Elt<DT>::T>(0);
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = to_f(t[i]);
-}
-
-template <int OUT> struct OutElt { using T = typename Elt<OUT>::T; };
-template <> struct OutElt<MAFAT_F8> { using T = uint8_t; };
-
-// V values of a piece to p, as OUT: bf16 rounds to nearest even, so does the
-// hardware's conversion to 8 bits (inputs are at most 448 or NaN here).
-template <int OUT, int V>
-__device__ __forceinline__ void store_piece(typename OutElt<OUT>::T* p, int n, const float (&v)[V]) {
-  typename OutElt<OUT>::T t[V];
-  if constexpr (OUT == MAFAT_F8) {
-    static_assert(V % 4 == 0, "four values a word");
-#pragma unroll
-    for (int i = 0; i < V; i += 4) {
-      int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[i], v[i + 1], 0, false);
-      w = __builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2], v[i + 3], w, true);
-      __builtin_memcpy(t + i, &w, 4);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) store1(&t[i], v[i]);
-  }
-  if (n >= V) {
-    __builtin_memcpy(p, t, sizeof(t));
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < n) p[i] = t[i];
-  }
-}
-
-// Over the TEAM threads of a row; all of them get the result.  Teams of more
-// than a wave join through LDS (the block is one team then).
-template <int TEAM, typename T, typename F>
-__device__ __forceinline__ T team_reduce(T v, F join, T* lds) {
-#pragma unroll
-  for (int o = (TEAM < 64 ? TEAM : 64) / 2; o > 0; o >>= 1) v = join(v, __shfl_xor(v, o, 64));
-  if constexpr (TEAM > 64) {
-    const int wave = static_cast<int>(threadIdx.x) >> 6;
-    if ((threadIdx.x & 63) == 0) lds[wave] = v;
-    __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int w = 1; w < TEAM / 64; ++w) v = join(v, lds[w]);
-  }
-  return v;
-}
-
-// The scale of a row from the bits of its largest magnitude, and what values
-// are multiplied by.  (Bits of magnitudes compare like the numbers, a NaN
-// above all: a maximum that lets no NaN pass unseen.)  Below 2^-100 the
-// reciprocal could overflow and the row is zero in 8 bits whatever its scale
-// is up to 1.
-__device__ __forceinline__ float row_scale(uint32_t most, float* inverse) {
-  const float m = __uint_as_float(most);
-  if (m < 0x1p-100f) {
-    *inverse = 1.f;
-    return 1.f;
-  }
-  *inverse = 448.f / m;
-  return m / 448.f;
-}
-
-struct Add {
-  __device__ float operator()(float a, float b) const { return a + b; }
-};
-struct MaxBits {
-  __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
-};
 
 // One row per team, NP pieces per thread at most.
 template <int DT, int OUT, bool RES, int TEAM, int NP>

@@ -102,4 +102,71 @@ hipError_t launch_cross(int dtype, const CrossArgs& a, const CrossPlan& p, hipSt
 hipError_t launch_cross_bf16(const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
 hipError_t launch_cross_f32(const CrossArgs& a, const CrossPlan& p, hipStream_t stream);
 
+struct RotaryArgs {
+  const int32_t* positions;
+  const double* turns;
+  const void* in[2];  // q and k
+  void* out[2];
+  int64_t in_row[2], in_head[2], out_row[2], out_head[2];
+  int64_t rows;
+  int32_t axes, q_heads, heads, head_dim, pairs;  // heads: of q and k together
+  int32_t turning, items;  // pieces of a head that turn, and all that are moved
+  int32_t heads_each;      // heads of a thread
+  float magnitude;
+};
+hipError_t launch_rotary(int dtype, bool interleaved, bool in_place, RotaryArgs a, hipStream_t stream);
+
+struct BlockArgs {
+  const void* x;
+  const void* gate;
+  const void* res;
+  const float* after_gain;
+  const float* scale;
+  const float* before_gain;
+  void* sum;
+  void* y;
+  float* y_scale;
+  int64_t x_stride, gate_stride, res_stride, sum_stride, y_stride;
+  int64_t rows;
+  int32_t cols, groups, part;  // part: columns of a group
+  int32_t after, before, silu;
+  float eps;
+};
+hipError_t launch_block_norm(int dtype, int out_dtype, const BlockArgs& a, hipStream_t stream);
+
+struct DecayArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* log_decay;
+  const int32_t* offsets;
+  float* states;
+  const int32_t* slots;
+  void* y;
+  // of requests cut into segments: [segments][kv_heads] states (first what a
+  // segment adds, then what it starts from) and factors of the segments
+  float* part;
+  float* factor;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, y_row, y_head, decay_row, state_slot;
+  int64_t pool;  // states of the pool
+  int32_t requests, rows, q_heads, kv_heads, group, key_dim, value_dim;
+  int32_t per_request;  // rows of a request, without offsets
+  int32_t decay_by_row;
+  int32_t segment;      // tokens of a segment
+  int32_t segments;     // of all requests together, at most
+  int32_t slices;       // blocks that share a state's columns
+  int32_t first_block;  // of this launch (see for_block_parts)
+  int32_t blocks;       // of all launches
+  float scale;
+};
+// How a call is cut up, from its sizes alone (the workspace depends on it).
+struct DecayPlan {
+  int recurrent;     // 1: token after token
+  int64_t segment;   // tokens of a segment, whole chunks
+  int64_t segments;  // of all requests together, at most
+  int split;         // 1: a request may have several
+};
+DecayPlan plan_decay(const mafat_decay& c);
+hipError_t launch_decay(int dtype, const DecayArgs& a, const DecayPlan& p, hipStream_t stream);
+
 }  // namespace mafat

@@ -1,0 +1,72 @@
+// reader_checks.h -- what the C entries of the reader's operators check their
+// arguments with (reader.cpp, tokens.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <initializer_list>
+#include <string>
+#include <utility>
+
+#include "mafat_internal.h"
+
+namespace mafat {
+namespace {
+
+constexpr int64_t kMax31 = int64_t{1} << 31;
+
+inline int fail(int status, const std::string& msg) {
+  set_error(msg);
+  return status;
+}
+
+inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+inline size_t elt_size(int dtype) { return dtype == MAFAT_F32 ? 4 : dtype == MAFAT_BF16 ? 2 : 1; }
+
+// Rows of `width` bytes every `pitch` bytes.
+struct Span {
+  const void* p;
+  int64_t rows;
+  int64_t width, pitch;
+};
+
+// Whether n rows of a stride have an extent that byte arithmetic can hold.
+inline bool fits(int64_t n, int64_t stride) { return n < 1 || stride < (int64_t{1} << 58) / n; }
+
+// Whether two tensors share a byte.  Tensors of one pitch may lie side by side
+// in the rows of one buffer; others count as overlapping if their extents do.
+inline bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return false;
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  const uintptr_t a1 = a0 + static_cast<uintptr_t>((a.rows - 1) * a.pitch + a.width);
+  const uintptr_t b1 = b0 + static_cast<uintptr_t>((b.rows - 1) * b.pitch + b.width);
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (a.pitch != b.pitch) return true;
+  const int64_t d = static_cast<int64_t>(b0 >= a0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch);
+  return d < a.width || d + b.width > a.pitch;
+}
+
+inline int launched(hipError_t e, const char* what) {
+  return e == hipSuccess ? MAFAT_OK : fail(MAFAT_EHIP, std::string(what) + " launch failed: " + hipGetErrorString(e));
+}
+
+// Heads and rows as one extent (strides in any order).
+inline Span extent(const void* p, int64_t esz, int64_t d, std::initializer_list<std::pair<int64_t, int64_t>> axes) {
+  int64_t n = d;
+  for (const auto& a : axes)
+    if (a.first > 0) n += (a.first - 1) * a.second;
+  return {p, 1, n * esz, n * esz};
+}
+
+// Rows of heads: rows of one pitch, which may lie side by side with others in
+// the rows of one buffer, where heads lie within a row; else one extent.
+inline Span rows_of_heads(const void* p, int64_t esz, int64_t d, int64_t rows, int64_t row, int64_t heads, int64_t head) {
+  const int64_t width = (heads - 1) * head + d;
+  if (rows <= 1 || row >= width) return {p, rows, width * esz, (rows <= 1 ? width : row) * esz};
+  return extent(p, esz, d, {{rows, row}, {heads, head}});
+}
+
+}  // namespace
+}  // namespace mafat

@@ -1,9 +1,10 @@
 """The operators of a reader (include/mafat_reader.h): a decoder whose tokens, of many requests at once, read the feature
 maps that a ``mafat.Network`` leaves on the device.
 
-``mafat_add_rms_norm``, ``mafat_linear`` and ``mafat_cross_attention`` keep the C names and only marshal arguments
-(device pointers and sizes).  ``add_rms_norm``, ``linear8`` and ``cross_attention`` take torch tensors on the GPU, check
-them, allocate what they return and run on the current stream of the tensors' device.  There is no fallback: every step
+``mafat_add_rms_norm``, ``mafat_linear``, ``mafat_cross_attention``, ``mafat_rotary``, ``mafat_decay_attention`` and
+``mafat_block_norm`` keep the C names and only marshal arguments (device pointers and sizes).  ``add_rms_norm``, ``linear8``,
+``cross_attention``, ``rotary``, ``decay_attention`` and ``block_norm`` take torch tensors on the GPU, check them, allocate
+what they return and run on the current stream of the tensors' device.  There is no fallback: every step
 runs in the library's HIP kernels.  They are forward only: a tensor that requires a gradient is refused while gradients are
 recorded (call under torch.no_grad(), or pass it detached).
 """
@@ -24,7 +25,7 @@ _NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, "f8": F8}
 
 # Every symbol include/mafat_reader.h declares.
 EXPORTS = ("mafat_add_rms_norm", "mafat_linear_workspace", "mafat_linear", "mafat_cross_workspace",
-           "mafat_cross_attention")
+           "mafat_cross_attention", "mafat_rotary", "mafat_block_norm", "mafat_decay_workspace", "mafat_decay_attention")
 
 
 class mafat_adapters(ctypes.Structure):
@@ -38,6 +39,28 @@ class mafat_cross(ctypes.Structure):
                 ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
                     "q_row", "q_head", "k_frame", "k_pos", "k_head", "v_frame", "v_pos", "v_head", "y_row", "y_head",
                     "mask_row")] + [("mask_by_row", ctypes.c_int32)]
+
+
+class mafat_turns(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("axes", ctypes.c_int32), ("rows", ctypes.c_int64), ("q_heads", ctypes.c_int32),
+                ("k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+                    "q_row", "q_head", "k_row", "k_head", "qy_row", "qy_head", "ky_row", "ky_head")]
+
+
+class mafat_block(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("after", ctypes.c_int32), ("groups", ctypes.c_int32), ("gate_act", ctypes.c_int32), ("before", ctypes.c_int32),
+                ("eps", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+                    "x_stride", "gate_stride", "residual_stride", "sum_stride", "y_stride")]
+
+
+class mafat_decay(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("requests", ctypes.c_int32), ("rows", ctypes.c_int64), ("slots", ctypes.c_int64),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("key_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32), ("scale", ctypes.c_float), ("decay_by_row", ctypes.c_int32)] + [
+                    (n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "y_row", "y_head",
+                                                  "decay_row", "state_slot")]
 
 
 _ready = None
@@ -56,6 +79,11 @@ def lib():
         crp = ctypes.POINTER(mafat_cross)
         L.mafat_cross_workspace.argtypes = [crp, ctypes.POINTER(sz)]
         L.mafat_cross_attention.argtypes = [crp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mafat_rotary.argtypes = [ctypes.POINTER(mafat_turns), vp, vp, vp, vp, vp, vp, vp]
+        L.mafat_block_norm.argtypes = [ctypes.POINTER(mafat_block), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        dcp = ctypes.POINTER(mafat_decay)
+        L.mafat_decay_workspace.argtypes = [dcp, ctypes.POINTER(sz)]
+        L.mafat_decay_attention.argtypes = [dcp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         _ready = L
     return _ready
 
@@ -168,6 +196,31 @@ def mafat_cross_attention(c, q, k, v, q_offsets, k_lengths, mask, y, lse, worksp
     """c: a mafat_cross; device pointers (int or None), stream: hipStream_t (int)."""
     M._check("mafat_cross_attention",
              lib().mafat_cross_attention(ctypes.byref(c), q, k, v, q_offsets, k_lengths, mask, y, lse, workspace, ws_bytes,
+                                         stream))
+
+
+def mafat_rotary(c, positions, turns, q, k, qy, ky, stream):
+    """c: a mafat_turns; device pointers (int or None), stream: hipStream_t (int)."""
+    M._check("mafat_rotary", lib().mafat_rotary(ctypes.byref(c), positions, turns, q, k, qy, ky, stream))
+
+
+def mafat_block_norm(c, x, after_gain, gate, scale, residual, total, before_gain, y, y_scale, stream):
+    """c: a mafat_block; device pointers (int or None), stream: hipStream_t (int)."""
+    M._check("mafat_block_norm", lib().mafat_block_norm(ctypes.byref(c), x, after_gain, gate, scale, residual, total,
+                                                        before_gain, y, y_scale, stream))
+
+
+def mafat_decay_workspace(c):
+    """Bytes of workspace of a mafat_decay."""
+    n = ctypes.c_size_t()
+    M._check("mafat_decay_workspace", lib().mafat_decay_workspace(ctypes.byref(c), ctypes.byref(n)))
+    return n.value
+
+
+def mafat_decay_attention(c, q, k, v, log_decay, offsets, states, slots, y, workspace, ws_bytes, stream):
+    """c: a mafat_decay; device pointers (int or None), stream: hipStream_t (int)."""
+    M._check("mafat_decay_attention",
+             lib().mafat_decay_attention(ctypes.byref(c), q, k, v, log_decay, offsets, states, slots, y, workspace, ws_bytes,
                                          stream))
 
 
@@ -314,4 +367,210 @@ def _cross_shape(dt, rows, hq, d, frames, positions, hkv, qs, ks, vs, scale, m_r
                     of(qs[0], rows, rows), of(qs[1], hq, rows), *(of(st[i], n, some) for st in (ks, vs) for i, n in (
                         (0, frames), (1, positions), (2, hkv))), hq * d, d, m_row, by_row)
     need = mafat_cross_workspace(c)
+    return ctypes.byref(c), need, c
+
+
+def rotary_turns(pairs, base=10000.0, stretch=1.0, trained=None, slow=1.0, fast=32.0, device="cuda"):
+    """Turns per step of `pairs` pairs (what rotary takes): base^(-i / pairs) / (2 pi), float64 [pairs].
+
+    stretch: by how much contexts are longer than trained ones; every frequency is divided by it.  With `trained`, the
+    trained length, only frequencies that turn less than `slow` times within it are, those that turn more than `fast` times
+    are kept, and in between the share goes linearly by the number of turns.
+    """
+    turns = base ** (-torch.arange(pairs, dtype=torch.float64, device=device) / max(pairs, 1)) / (2 * math.pi)
+    if trained is None:
+        return turns / stretch
+    keep = ((turns * trained - slow) / (fast - slow)).clamp(0, 1)
+    return turns * (keep + (1 - keep) / stretch)
+
+
+def rotary(q, positions, turns, k=None, interleaved=False, magnitude=1.0, in_place=False):
+    """(q', k'): q and k with the first pairs of every head turned by their row's position (k' is None without k).
+
+    q: [rows, q_heads, d] and k: [rows, k_heads, d], float32 or bfloat16, of any row and head strides (e.g. parts of one
+    projection's rows).  positions: int32 [rows] or [rows, axes].  turns: float64 [pairs] or [axes, pairs], turns per step
+    (rotary_turns); pair i turns by 2 pi sum_a positions[:, a] turns[a, i].  A pair is values i and pairs + i, or, interleaved,
+    2 i and 2 i + 1; values behind the pairs stay as they are.  magnitude: a factor of the turned values.  in_place: q and k
+    are overwritten and returned.
+    """
+    dt = q.dtype
+    if not q.is_cuda or q.dim() != 3 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
+    if _recording() and (q.requires_grad or _wants_grad(k) or turns.requires_grad or getattr(magnitude, "requires_grad", False)):
+        _forward_only()
+    rows, hq, d = q.shape
+    dev, hk, ks = q.device, 0, None
+    if k is not None:
+        if k.dim() != 3 or k.dtype is not dt or k.device != dev or k.shape[0] != rows or k.shape[2] != d or k.shape[1] < 1:
+            _refuse(f"k must be a {dt} tensor [{rows}, heads, {d}] on {dev}")
+        hk, ks = k.shape[1], k.stride()
+    axes = positions.shape[1] if positions.dim() == 2 else 1
+    if positions.dtype is not torch.int32 or positions.shape not in ((rows,), (rows, axes)) or positions.device != dev or \
+            not positions.is_contiguous():
+        _refuse(f"positions must be a contiguous int32 tensor [{rows}] or [{rows}, axes] on {dev}")
+    pairs = turns.shape[-1] if turns.dim() else 0
+    if turns.dtype is not torch.float64 or turns.shape not in ((axes, pairs), (pairs,) if axes == 1 else None) or \
+            turns.device != dev or not turns.is_contiguous():
+        _refuse(f"turns must be a contiguous float64 tensor [{axes}, pairs] on {dev}")
+    ref, _ = _rotary_shape(dt, rows, hq, hk, d, axes, pairs, bool(interleaved), float(magnitude), q.stride(), ks, bool(in_place))
+    if in_place:
+        qy, ky = q, k
+    else:
+        qy = torch.empty((rows, hq, d), dtype=dt, device=dev)
+        ky = None if k is None else torch.empty((rows, hk, d), dtype=dt, device=dev)
+    _call("mafat_rotary", dev.index, ref, positions.data_ptr(), turns.data_ptr(), q.data_ptr(), _ptr(k), qy.data_ptr(), _ptr(ky))
+    return qy, ky
+
+
+def _outer(stride, n, entries, width):
+    """The stride of an axis of n entries (one of a single entry, or of a tensor without entries, may have any)."""
+    return stride if n > 1 and entries else max(stride, width)
+
+
+@functools.lru_cache(maxsize=256)
+def _rotary_shape(dt, rows, hq, hk, d, axes, pairs, interleaved, magnitude, qs, ks, in_place):
+    """(reference to the call's mafat_turns, the struct itself) for sizes and strides."""
+    if hq < 1 or d < 1:
+        _refuse("q must have heads and values")
+    if d > 1 and (qs[2] != 1 or (ks is not None and ks[2] != 1)):
+        _refuse("q and k must have contiguous values of a head")
+    q = _outer(qs[0], rows, rows, d), _outer(qs[1], hq, rows, d)
+    k = (_outer(ks[0], rows, rows, d), _outer(ks[1], hk, rows, d)) if ks is not None else (d, d)
+    out = (*q, *k) if in_place else (hq * d, d, max(hk, 1) * d, d)
+    c = mafat_turns(_CODES[dt], axes, rows, hq, hk, d, pairs, interleaved, magnitude, *q, *k, *out)
+    return ctypes.byref(c), c
+
+
+def block_norm(x, after=True, after_gain=None, groups=1, gate=None, act="silu", scale=None, residual=None, before=True,
+               before_gain=None, eps=1e-6, out="f8"):
+    """(h, y, y_scale): a block's output x on its way into the residual stream and the next block.
+
+        u = x / sqrt(mean(x^2) + eps) * after_gain      if after, the mean over each of `groups` equal parts of a row
+        u = u * act(gate)                               with a gate; act: "silu" (gate * sigmoid(gate)) or "sigmoid"
+        h = residual + scale * u
+        y = h / sqrt(mean(h^2) + eps) * before_gain     if before
+
+    x, gate, residual: [rows, cols], float32 or bfloat16 alike, contiguous rows of any stride.  after_gain, scale,
+    before_gain: float32 [cols] or None (ones).  h comes back in x's type (None without a residual); y follows from h before
+    that rounding.  out and y_scale as for add_rms_norm.
+    """
+    dt, to = x.dtype, _NAMES.get(out)
+    if not x.is_cuda or x.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        _refuse("x must be a float32 or bfloat16 matrix on the GPU")
+    if _recording() and (x.requires_grad or _wants_grad(after_gain) or _wants_grad(gate) or _wants_grad(scale) or
+                         _wants_grad(residual) or _wants_grad(before_gain)):
+        _forward_only()
+    if to is None:
+        _refuse(f"out must be one of {sorted(_NAMES)}, not {out!r}")
+    if act != "silu" and act != "sigmoid":
+        _refuse(f"act must be 'silu' or 'sigmoid', not {act!r}")
+    rows, cols = shape = x.shape
+    if cols < 1:
+        _refuse("x has no columns")
+    dev = x.device
+    x_stride = _row_stride(x, "x")
+    after_at = _vector(after_gain, cols, torch.float32, dev, "after_gain")
+    before_at = _vector(before_gain, cols, torch.float32, dev, "before_gain")
+    scale_at = _vector(scale, cols, torch.float32, dev, "scale")
+    h = h_at = res_at = gate_at = y_scale = y_scale_at = None
+    g_stride = r_stride = cols
+    if gate is not None:
+        g_stride = _matrix(gate, shape, dt, dev, "gate")
+        gate_at = gate.data_ptr()
+    if residual is not None:
+        r_stride = _matrix(residual, shape, dt, dev, "residual")
+        h = torch.empty((rows, cols), dtype=dt, device=dev)
+        h_at, res_at = h.data_ptr(), residual.data_ptr()
+    y = torch.empty((rows, cols), dtype=to, device=dev)
+    if to is F8:
+        y_scale = torch.empty(rows, dtype=torch.float32, device=dev)
+        y_scale_at = y_scale.data_ptr()
+    ref, _ = _block_shape(dt, to, rows, cols, bool(after), groups, act == "silu", bool(before), eps, x_stride, g_stride, r_stride)
+    _call("mafat_block_norm", dev.index, ref, x.data_ptr(), after_at, gate_at, scale_at, res_at, h_at, before_at, y.data_ptr(),
+          y_scale_at)
+    return h, y, y_scale
+
+
+@functools.lru_cache(maxsize=256)
+def _block_shape(dt, to, rows, cols, after, groups, silu, before, eps, x_stride, g_stride, r_stride):
+    """(reference to the call's mafat_block, the struct itself)."""
+    c = mafat_block(_CODES[dt], _CODES[to], rows, cols, after, groups, silu, before, eps, x_stride, g_stride, r_stride, cols, cols)
+    return ctypes.byref(c), c
+
+
+def decay_attention(q, k, v, log_decay, states=None, slots=None, offsets=None, scale=None):
+    """y: linear attention among the tokens of each request, with a decay for each head; [rows, q_heads, dv] in q's type.
+
+        S_t = exp(log_decay_t) S_(t-1) + k_t v_t^T,  y_t = scale * q_t S_t
+
+    q: [rows, q_heads, dk], k: [rows, kv_heads, dk], v: [rows, kv_heads, dv], the tokens of request 0, then those of request
+    1, ..., all float32 or all bfloat16, strides free but for the last; q_heads a multiple of kv_heads, dk and dv up to 256.
+    log_decay: float32 [kv_heads] or [rows, kv_heads], at most 0 (above counts as 0).  states: float32 [slots, kv_heads, dk, dv],
+    where each request's state is read from and, updated, kept in place (None: zeros, and nothing is kept); slots: int32
+    [requests], each request's state (outside [0, slots): zeros, not kept; one that an earlier request has: y is NaN and
+    the state is that request's), None: request i has state i.  offsets: int32 [requests + 1], request i's rows are offsets[i]
+    to offsets[i + 1] (None: as many each; rows that no request has come back undefined).  The number of requests is that of
+    offsets, of slots, of states, or 1.  scale: a number (None: 1 / sqrt(dk)).
+    """
+    dt = q.dtype
+    if not q.is_cuda or q.dim() != 3 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
+                         _wants_grad(states) or getattr(scale, "requires_grad", False)):
+        _forward_only()
+    rows, hq, dk = q.shape
+    dev = q.device
+    if k.dim() != 3 or k.dtype is not dt or k.device != dev or k.shape[0] != rows or k.shape[2] != dk:
+        _refuse(f"k must be a {dt} tensor [{rows}, heads, {dk}] on {dev}")
+    hkv = k.shape[1]
+    if v.dim() != 3 or v.dtype is not dt or v.device != dev or v.shape[:2] != (rows, hkv):
+        _refuse(f"v must be a {dt} tensor [{rows}, {hkv}, d] on {dev}")
+    dv = v.shape[2]
+    by_row = log_decay.dim() == 2
+    if log_decay.dtype is not torch.float32 or log_decay.device != dev or log_decay.shape != ((rows, hkv) if by_row else (hkv,)):
+        _refuse(f"log_decay must be a float32 tensor [{hkv}] or [{rows}, {hkv}] on {dev}")
+    d_row = _row_stride(log_decay, "log_decay") if by_row else hkv
+    if not by_row and hkv > 1 and log_decay.stride(0) != 1:
+        _refuse("log_decay must be contiguous")
+    pool, states_at, s_slot = 0, None, hkv * dk * dv
+    if states is not None:
+        if states.dtype is not torch.float32 or states.device != dev or states.dim() != 4 or states.shape[1:] != (hkv, dk, dv):
+            _refuse(f"states must be a float32 tensor [slots, {hkv}, {dk}, {dv}] on {dev}")
+        pool = states.shape[0]
+        if pool and not states[0].is_contiguous():
+            _refuse("states must be contiguous but for their first axis")
+        states_at = states.data_ptr()
+        s_slot = _outer(states.stride(0), pool, pool, s_slot)
+    if offsets is not None:
+        requests = offsets.numel() - 1
+    elif slots is not None:
+        requests = slots.numel()
+    else:
+        requests = pool if states is not None else 1
+    if slots is not None and states is None:
+        _refuse("slots need states")
+    offsets_at = _vector(offsets, requests + 1, torch.int32, dev, "offsets")
+    slots_at = _vector(slots, requests, torch.int32, dev, "slots")
+    if scale is not None:
+        scale = float(scale)  # of a tensor its value now: the shapes below are kept by what they hold
+    ref, need, _ = _decay_shape(dt, requests, rows, pool, hq, hkv, dk, dv, scale, by_row, q.stride(), k.stride(), v.stride(), d_row,
+                                s_slot)
+    y = torch.empty((rows, hq, dv), dtype=dt, device=dev)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call("mafat_decay_attention", dev.index, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), offsets_at,
+          states_at, slots_at, y.data_ptr(), _ptr(ws), need)
+    return y
+
+
+@functools.lru_cache(maxsize=256)
+def _decay_shape(dt, requests, rows, pool, hq, hkv, dk, dv, scale, by_row, qs, ks, vs, d_row, s_slot):
+    """(reference to the call's mafat_decay, bytes of workspace, the struct itself) for sizes and strides."""
+    if not (requests > 0 and hkv > 0 and hq > 0 and dk > 0 and dv > 0 and hq % hkv == 0):
+        _refuse("there must be requests, heads and values, q's heads a multiple of k's")
+    if (dk > 1 and not qs[2] == ks[2] == 1) or (dv > 1 and vs[2] != 1):
+        _refuse("q, k and v must have contiguous values of a head")
+    axes = [_outer(st[i], n, rows, d) for st, h, d in ((qs, hq, dk), (ks, hkv, dk), (vs, hkv, dv)) for i, n in ((0, rows), (1, h))]
+    c = mafat_decay(_CODES[dt], requests, rows, pool, hq, hkv, dk, dv, 1 / math.sqrt(dk) if scale is None else scale, by_row, *axes,
+                    hq * dv, dv, d_row, s_slot)
+    need = mafat_decay_workspace(c)
     return ctypes.byref(c), need, c
