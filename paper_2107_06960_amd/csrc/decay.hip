@@ -15,6 +15,7 @@
 // forms what each segment adds to the state, a second one turns these into the
 // states that the segments start from, the last one gives the outputs.
 #include "decay_device.h"
+#include "decay_launch.h"
 
 namespace mafat {
 namespace {
@@ -100,10 +101,6 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
 
 // ------------------------------------------------------------ prompts, any size
 
-// What a launch of the chunked kernels does: what a segment adds to the state,
-// or the outputs (and the last state).
-enum { ADDS = 0, OUTPUTS = 1 };
-
 // Any size, stride, alignment and type: 32 tokens at a time as float32 in LDS
 // and on the float32 matrix instructions (bfloat16 values are exact there).  A
 // block has 64 columns of the state, a wave 16 of them in KT tiles of 16 rows.
@@ -116,9 +113,9 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   using T = typename Elt<DT>::T;
   constexpr int C = 32, KP = 16 * KT + 4, VP = 68, PP = 36;  // tokens; floats of a row of LDS
   __shared__ __align__(16) float sk[C * KP];
-  __shared__ __align__(16) float sq[MODE == OUTPUTS ? C * KP : 4];
+  __shared__ __align__(16) float sq[MODE == DECAY_OUTPUTS ? C * KP : 4];
   __shared__ __align__(16) float sv[C * VP];
-  __shared__ __align__(16) float sp[MODE == OUTPUTS ? C * PP : 4];
+  __shared__ __align__(16) float sp[MODE == DECAY_OUTPUTS ? C * PP : 4];
   __shared__ double sc[C];
   __shared__ int odd;  // whether the chunk's values are not all finite
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
@@ -129,14 +126,14 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = bh - b * a.kv_heads;
   const Segment seg = find_segment(a, b);
-  if (!seg.any || (MODE == ADDS && seg.index + 1 == seg.count)) return;
+  if (!seg.any || (MODE == DECAY_ADDS && seg.index + 1 == seg.count)) return;
   const int c0 = 64 * slice, col = c0 + 16 * wave + l16;  // of the state
-  const int64_t slot = MODE == OUTPUTS && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
+  const int64_t slot = MODE == DECAY_OUTPUTS && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
   float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
 
   f32x4 s[KT];
-  if (MODE == OUTPUTS && (kept || seg.count > 1)) {
+  if (MODE == DECAY_OUTPUTS && (kept || seg.count > 1)) {
     const float* from = seg.count > 1 ? part : kept;
 #pragma unroll
     for (int i = 0; i < KT; ++i)
@@ -181,7 +178,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
       if (lane < C) sc[lane] = g;
     }
     __syncthreads();
-    if constexpr (MODE == OUTPUTS) {
+    if constexpr (MODE == DECAY_OUTPUTS) {
       for (int h = 0; h < a.group; ++h) {
         const int head = kv * a.group + h;
         for (int e = tid; e < C * 4 * KT; e += 256) {
@@ -270,7 +267,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
         for (int i = 0; i < KT; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(sk[j * KP + 16 * i + l16], v, s[i], 0, 0, 0);
       }
   }
-  float* const to = MODE == ADDS ? part : seg.index + 1 == seg.count ? kept : nullptr;
+  float* const to = MODE == DECAY_ADDS ? part : seg.index + 1 == seg.count ? kept : nullptr;
   if (to) {
 #pragma unroll
     for (int i = 0; i < KT; ++i)
@@ -280,7 +277,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
         if (row < a.key_dim && col < a.value_dim) to[static_cast<int64_t>(row) * a.value_dim + col] = s[i][r];
       }
   }
-  if (MODE == ADDS && slice == 0 && tid == 0)
+  if (MODE == DECAY_ADDS && slice == 0 && tid == 0)
     a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
 }
 
@@ -338,16 +335,13 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
 }
 
 template <int DT, int MODE>
-hipError_t launch_any(DecayArgs a, hipStream_t stream) {
+hipError_t launch_chunks(DecayArgs a, hipStream_t stream) {
+  if (DT == MAFAT_BF16 && decay_bf16_fits(a)) return launch_decay_bf16(MODE, a, stream);
   a.slices = (a.value_dim + 63) / 64;
-  const int64_t blocks = static_cast<int64_t>(a.segments) * a.kv_heads * a.slices;
-  if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
-  a.blocks = static_cast<int32_t>(blocks);
-  return for_block_parts(blocks, [&](int32_t from, unsigned n) {
-    a.first_block = from;
-    if (a.key_dim <= 64) hipLaunchKernelGGL((decay_any_kernel<DT, 4, MODE>), dim3(n), dim3(256), 0, stream, a);
-    else if (a.key_dim <= 128) hipLaunchKernelGGL((decay_any_kernel<DT, 8, MODE>), dim3(n), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((decay_any_kernel<DT, 16, MODE>), dim3(n), dim3(256), 0, stream, a);
+  return for_decay_blocks(a, [&](const DecayArgs& p, unsigned n) {
+    if (a.key_dim <= 64) hipLaunchKernelGGL((decay_any_kernel<DT, 4, MODE>), dim3(n), dim3(256), 0, stream, p);
+    else if (a.key_dim <= 128) hipLaunchKernelGGL((decay_any_kernel<DT, 8, MODE>), dim3(n), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((decay_any_kernel<DT, 16, MODE>), dim3(n), dim3(256), 0, stream, p);
   });
 }
 
@@ -378,11 +372,11 @@ hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
   if (p.recurrent) return launch_step<DT>(a, stream);
   // (without offsets the requests' lengths are known)
   if (p.split && (a.offsets || a.per_request > a.segment)) {
-    hipError_t e = launch_any<DT, ADDS>(a, stream);
+    hipError_t e = launch_chunks<DT, DECAY_ADDS>(a, stream);
     if (e == hipSuccess) e = launch_join(a, stream);
     if (e != hipSuccess) return e;
   }
-  return launch_any<DT, OUTPUTS>(a, stream);
+  return launch_chunks<DT, DECAY_OUTPUTS>(a, stream);
 }
 
 }  // namespace
@@ -391,10 +385,14 @@ DecayPlan plan_decay(const mafat_decay& c) {
   DecayPlan p{};
   // One or two tokens a request, if they are alike: a chunk would be nearly empty.
   p.recurrent = c.rows <= 2 * int64_t{c.requests};
-  // Segments that leave about two blocks a CU, of 256 tokens at least.
-  const int64_t slices = (c.value_dim + 63) / 64;
-  int64_t len = (c.rows * c.kv_heads * slices + 511) / 512;
-  len = len < 256 ? 256 : (len + 63) / 64 * 64;
+  // Segments of 256 tokens at least that leave two blocks a CU, all of them at once: one
+  // more would make the call take twice as long.  A request adds a segment that is not
+  // full.  With that many requests alone, twice their mean length.
+  const int columns = c.dtype == MAFAT_BF16 && c.key_dim % 8 == 0 && c.value_dim % 8 == 0 ? 128 : 64;  // of a block, mostly
+  const int64_t slices = (c.value_dim + columns - 1) / columns;
+  const int64_t most = 512 / (c.kv_heads * slices);
+  int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
+  len = len < 256 ? 256 : (len + 31) / 32 * 32;
   p.segment = len;
   p.segments = c.rows / len + c.requests;
   p.split = !p.recurrent && c.rows > len;

@@ -1,0 +1,463 @@
+// decay_bf16.hip -- linear attention with decays in bfloat16, heads of whole
+// 16-byte pieces: chunks of 32 tokens on the matrix cores (see decay.hip for the
+// scheme, and for anything else).
+//
+// A block has the chunks of a segment of one request and key/value head, a wave 32
+// columns of its state.  With S^T = K Q^T, O^T = S_0^T Q^T + V^T P^T and
+// S += K^T V no product needs an exchange between lanes: the 32x32 instruction's
+// result has, in lane l, column l % 32 and rows 8 g + 4 (l / 32) + b in register
+// 4 g + b, and an operand takes 8 entries of the summed axis a lane and step.
+// Scores come out as the operand that V^T P^T takes, and the state as the one
+// that S_0^T Q^T takes: K^T's rows are read in the order that makes a lane's 8
+// entries those that a 16-byte piece of a query holds (see dk_of).
+// Every wave forms all of the chunk's scores, 8 of its matrix instructions at
+// key_dim 128, which costs less than a barrier and a pass through LDS.
+//
+// The state is kept relative to a factor 2^A: S = 2^A S', A the logarithm of
+// the decays since it was last brought up to date.  With v'_j = 2^(-A - c_j) v_j
+//   y_i = scale 2^(A + c_i) (q_i S' + sum_{j <= i} (q_i . k_j) v'_j),  S' += sum_j k_j v'_j^T
+// so a chunk takes no exponentials but one a token, and no product of the whole
+// state.  S' is multiplied by 2^A and A set to zero when A + c_C would pass
+// -kLag: float32 and bfloat16 have room for the factor.  A chunk that forgets
+// more than that by itself takes exponentials of differences, as decay.hip says.
+//
+// What a state or a weighted value loses in bfloat16 goes along as further
+// bfloat16 parts: the states that are kept and joined are float32 and have to be
+// near float32's accuracy after any number of chunks (three parts of a value:
+// 2^-27 of it; two of the states that rows read).  Scores are rounded once: they
+// end in an output that is rounded alike.
+#include "cross_fast.h"
+#include "decay_device.h"
+#include "decay_launch.h"
+
+namespace mafat {
+namespace {
+
+constexpr int C = 32;         // tokens of a chunk
+constexpr double kLag = 24.0;  // of A, in base 2
+
+// Byte offset of row r in a tile of PITCH-byte rows; position p of a row holds
+// the 16-byte piece p ^ turn(r).  Reads of a row per lane (16 lanes at a time)
+// and transposing reads (32 lanes at a time: 64 bytes of each of 4 rows)
+// meet every bank once.
+template <int PITCH>
+__device__ __forceinline__ int turn(int r) {
+  return PITCH == 128 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
+}
+
+// A tile of C rows straight into LDS: each wave its loads of 1 KB.
+template <int PITCH, int NW>
+struct TileFetch {
+  static constexpr int PER = PITCH / 16, ROWS = 64 / PER, LOADS = C / ROWS / NW;
+  static_assert(LOADS * ROWS * NW == C, "whole loads per wave");
+  const uint16_t* base;
+  int row, dim;
+  unsigned off[LOADS];
+  __device__ __forceinline__ void start(const void* p, int64_t offset, int64_t stride, int d, int wave) {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    base = static_cast<const uint16_t*>(p) + offset;
+    row = static_cast<int>(stride);
+    dim = d;
+#pragma unroll
+    for (int g = 0; g < LOADS; ++g) {
+      const int r = ROWS * (g * NW + wave) + lane / PER;
+      const int at = 8 * ((lane % PER) ^ turn<PITCH>(r));
+      off[g] = at < d ? static_cast<unsigned>(2 * (r * row + at)) : 0x80000000u;
+    }
+  }
+  // n rows from row0 on (the others read as zeros) to byte `to` of LDS.
+  __device__ __forceinline__ void issue(int64_t row0, int n, unsigned to, int wave) const {
+    const u32x4 range = range_of(base + row0 * row, static_cast<unsigned>(2 * ((n - 1) * row + dim)));
+#pragma unroll
+    for (int g = 0; g < LOADS; ++g) load_to_lds(range, off[g], to + ROWS * (g * NW + wave) * PITCH);
+  }
+};
+
+// Entry of the keys that register r of tile t holds in lanes of half h.
+__device__ __forceinline__ int dk_of(int t, int r, int h) { return 32 * t + 16 * (r >> 3) + 8 * h + (r & 7); }
+
+__device__ __forceinline__ float lower(uint32_t two) { return __uint_as_float(two << 16); }
+__device__ __forceinline__ float upper(uint32_t two) { return __uint_as_float(two & 0xffff0000u); }
+// Two values as the sum of N bfloat16 parts each, the largest first.
+template <int N>
+__device__ __forceinline__ void split(float x, float y, uint32_t (&part)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    part[i] = pack_bf16(x, y);
+    x -= lower(part[i]);
+    y -= upper(part[i]);
+  }
+}
+
+// Waits for all loads, also as the compiler counts them: one that it takes for
+// pending in a loop would have it wait there for the loads into LDS too.
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0) alone
+  wait_vmcnt<0>();
+}
+
+// v of the lane `STEP` before in the row of 16 lanes (0 for the first ones).
+template <int STEP>
+__device__ __forceinline__ double from_left(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(u)), 0x110 + STEP, 15, 15, true));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(u >> 32)), 0x110 + STEP, 15, 15, true));
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(u)), lane));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(u >> 32)), lane));
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+// Sums over lanes l % 32 up to each one, of values that both halves of the wave
+// have, and the sum of all.
+__device__ __forceinline__ double scan32(double v, double* all) {
+  v += from_left<1>(v);
+  v += from_left<2>(v);
+  v += from_left<4>(v);
+  v += from_left<8>(v);
+  const double first = lane_value(v, 15);
+  v += threadIdx.x & 16 ? first : 0.0;
+  *all = lane_value(v, 31);
+  return v;
+}
+
+template <int KP, int NW, int MODE>
+__global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
+  constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
+  constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH;
+  constexpr bool OUT = MODE == DECAY_OUTPUTS;
+  __shared__ __align__(1024) unsigned char smem[2 * (KTILE + VTILE + (OUT ? KTILE : 0))];
+  __shared__ __align__(16) float table[NW][2][C];  // of each wave: c_j, and the values' weights
+  const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.blocks);
+  const int bh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.slices));
+  const int slice = id - bh * a.slices;
+  const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
+  const int kv = bh - b * a.kv_heads;
+  const Segment seg = find_segment(a, b);
+  if (!seg.any || (!OUT && seg.index + 1 == seg.count)) return;
+
+  const int c0 = 32 * NW * slice, col = c0 + 32 * wave + c;  // of the state
+  const int chunks = (seg.n + C - 1) / C;
+  unsigned char* const sk = smem;
+  unsigned char* const sv = smem + 2 * KTILE;
+  unsigned char* const sq = smem + 2 * (KTILE + VTILE);
+  TileFetch<KPITCH, NW> fk, fq;
+  TileFetch<VPITCH, NW> fv;
+  fk.start(a.k, seg.first * a.k_row + kv * a.k_head, a.k_row, a.key_dim, wave);
+  fv.start(a.v, seg.first * a.v_row + kv * a.v_head + c0, a.v_row, a.value_dim - c0, wave);
+  const float* const decays = a.log_decay + (a.decay_by_row ? seg.first * a.decay_row : 0) + kv;
+  auto issue_kv = [&](int t) {
+    const int n = min(C, seg.n - t * C);
+    fk.issue(static_cast<int64_t>(t) * C, n, lds_offset(sk) + (t & 1) * KTILE, wave);
+    fv.issue(static_cast<int64_t>(t) * C, n, lds_offset(sv) + (t & 1) * VTILE, wave);
+  };
+  // Head g of the group, chunk t; `at` counts both.
+  auto issue_q = [&](int t, int g, int at) {
+    fq.base = static_cast<const uint16_t*>(a.q) + seg.first * a.q_row + (kv * a.group + g) * a.q_head;
+    fq.issue(static_cast<int64_t>(t) * C, min(C, seg.n - t * C), lds_offset(sq) + (at & 1) * KTILE, wave);
+  };
+  issue_kv(0);
+  if constexpr (OUT) {
+    fq.start(a.q, 0, a.q_row, a.key_dim, wave);
+    issue_q(0, 0, 0);
+  }
+  float next_decay = 0.f;  // of token c of the next chunk
+  auto ask_decay = [&](int t) {
+    const int i = t * C + c;
+    next_decay = i < seg.n ? decays[a.decay_by_row ? i * a.decay_row : 0] : 0.f;
+  };
+  ask_decay(0);
+
+  const int64_t slot = OUT && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
+  float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
+  float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
+  f32x16 s[KT];
+  if (OUT && (kept || seg.count > 1)) {
+    const float* from = seg.count > 1 ? part : kept;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = dk_of(t, r, h);
+        s[t][r] = row < a.key_dim && col < a.value_dim ? from[static_cast<int64_t>(row) * a.value_dim + col] : 0.f;
+      }
+  } else {
+    const float f = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[t][r] = f;
+  }
+
+  // LDS offsets of the fragments
+  const int row_at = c * KPITCH + ((h ^ turn<KPITCH>(c)) << 4);  // ^ (step << 5)
+  const int tr = 4 * h + ((lane & 15) >> 2), f = lane & 3, half16 = (lane >> 4) & 1;
+  const int kp = 2 * half16 + (f & 1), vp = 2 * half16 + (f >> 1);  // 16-byte piece of a 64-byte quarter
+  const int k_lo = tr * KPITCH + ((kp ^ turn<KPITCH>(tr)) << 4), k_hi = (tr + 8) * KPITCH + ((kp ^ turn<KPITCH>(tr + 8)) << 4);
+  const int k_half = 8 * (f >> 1);
+  const int v_lo = tr * VPITCH + (((4 * wave + vp) ^ turn<VPITCH>(tr)) << 4) + 8 * (f & 1);
+  const int v_hi = (tr + 8) * VPITCH + (((4 * wave + vp) ^ turn<VPITCH>(tr + 8)) << 4) + 8 * (f & 1);
+  // Pairs of a lane's scores that are not above the diagonal (as bits, for what
+  // is there need not be finite).
+  uint32_t below[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int j = 8 * (i >> 1) + 4 * h + 2 * (i & 1);
+    below[i] = (j <= c ? 0xffffu : 0u) | (j + 1 <= c ? 0xffff0000u : 0u);
+  }
+  float* const tc = table[wave][0];
+  float* const tw = table[wave][1];
+
+  wait_loads();
+  double total = 0.0, lag = 0.0;  // of the segment's decays, in base 2; A
+  int at = 0;          // chunks and heads so far
+  u32x4 done[2] = {};  // outputs of the last chunk, still to be written
+  uint16_t* done_at = nullptr;
+  auto write_done = [&] {
+    if (done_at) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (c0 + 32 * wave + 16 * i + 8 * h < a.value_dim) __builtin_memcpy(done_at + 16 * i, &done[i], 16);
+    }
+  };
+  auto times = [&](double log2) {
+    const float by = __builtin_amdgcn_exp2f(static_cast<float>(log2));
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[t][r] *= by;
+  };
+  for (int t = 0; t < chunks; ++t) {
+    const int n = min(C, seg.n - t * C);
+    double all = 0.0;                       // c_C
+    float c_here = 0.f, e_here = 0.f;       // c_i of token i = c, and 2^(A + c_i)
+    bool steep = false;                     // exponentials of differences
+    u32x4 vf[2];
+    bool odd = false;
+    const int heads = OUT ? a.group : 1;
+    for (int g = 0; g < heads; ++g, ++at) {
+      // Everything asked for an iteration ago is there, and its outputs are written.
+      wait_loads();
+      wg_barrier_writes();  // for all waves, and nobody reads the other slots any more
+      // (The compiler waits for the decay where it is first used, and knows
+      // nothing of the loads into LDS: before they are asked for.)
+      float decay = next_decay;
+      asm volatile("" : "+v"(decay));
+      if constexpr (OUT) write_done();
+      const bool more = t + 1 < chunks;
+      if (g + 1 < heads) {
+        issue_q(t, g + 1, at + 1);
+      } else if (more) {
+        issue_kv(t + 1);
+        if constexpr (OUT) issue_q(t + 1, 0, at + 1);
+      }
+      const unsigned char* k = sk + (t & 1) * KTILE;
+      if (g == 0) {
+        if (more) ask_decay(t + 1);
+        const double step = c < n || !a.decay_by_row ? static_cast<double>(decay_log2(decay)) : 0.0;
+        double ci;
+        if (a.decay_by_row) {
+          ci = scan32(step, &all);
+        } else {  // (token 0 is there, and all tokens have its decay)
+          const double one = lane_value(step, 0);
+          ci = min(c + 1, n) * one;
+          all = n * one;
+        }
+        total += all;
+        if (!(lag + all >= -kLag)) {
+          times(lag);
+          lag = 0.0;
+          steep = !(all >= -kLag);
+        }
+        c_here = static_cast<float>(ci);
+        e_here = __builtin_amdgcn_exp2f(static_cast<float>(lag + ci));
+        tc[c] = c_here;
+        tw[c] = __builtin_amdgcn_exp2f(static_cast<float>(steep ? all - ci : -lag - ci));
+        const unsigned char* v = sv + (t & 1) * VTILE;
+        uint32_t bad = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const s16x4 two[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + v_lo + 16 * u * VPITCH)),
+                                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + v_hi + 16 * u * VPITCH))};
+          vf[u] = __builtin_bit_cast(u32x4, two);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bad |= (vf[u][i] & 0x7f807f80u) + 0x00800080u;  // exponents of ones carry
+        }
+        if constexpr (OUT) odd = __builtin_amdgcn_ballot_w64((bad & 0x80008000u) != 0) != 0;
+      }
+      f32x16 p, o;
+      if constexpr (OUT) {
+        const unsigned char* q = sq + (at & 1) * KTILE;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = o[i] = 0.f;
+#pragma unroll
+        for (int x = 0; x < STEPS; ++x) {
+          const u32x4 qf = *reinterpret_cast<const u32x4*>(q + (row_at ^ (x << 5)));
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(k + (row_at ^ (x << 5)));
+          u32x4 sp[2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t two[2];
+            split(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1], two);
+            sp[0][i] = two[0];
+            sp[1][i] = two[1];
+          }
+          Tile<MAFAT_BF16>::mul(p, kf, qf);
+          Tile<MAFAT_BF16>::mul(o, sp[0], qf);
+          Tile<MAFAT_BF16>::mul(o, sp[1], qf);
+        }
+      }
+      // the values, weighted
+      u32x4 vp3[3][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(tw + 16 * u + 8 * i + 4 * h);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            uint32_t part3[3];
+            split(lower(vf[u][2 * i + x]) * w[2 * x], upper(vf[u][2 * i + x]) * w[2 * x + 1], part3);
+#pragma unroll
+            for (int y = 0; y < 3; ++y) vp3[y][u][2 * i + x] = part3[y];
+          }
+        }
+      if constexpr (OUT) {
+        uint32_t pp[8];
+        if (steep) {
+          // c_i and c_j as float32: off by 2^-24 of their size, at most 6400, far
+          // below the scores' rounding
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + 4 * h);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p[4 * i + x] *= __builtin_amdgcn_exp2f(c_here - cj[x]);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] *= e_here;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pp[i] = pack_bf16(p[2 * i], p[2 * i + 1]) & below[i];
+        // Values of one part as they are, or weighted ones in two.
+        const int parts = steep ? 1 : 2;
+        u32x4 vo[2][2] = {{vf[0], vf[1]}, {vp3[1][0], vp3[1][1]}};
+        if (!steep) {
+          vo[0][0] = vp3[0][0];
+          vo[0][1] = vp3[0][1];
+        }
+        if (!odd) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) Tile<MAFAT_BF16>::mul(o, vo[0][u], u32x4{pp[4 * u], pp[4 * u + 1], pp[4 * u + 2], pp[4 * u + 3]});
+          if (!steep) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) Tile<MAFAT_BF16>::mul(o, vo[1][u], u32x4{pp[4 * u], pp[4 * u + 1], pp[4 * u + 2], pp[4 * u + 3]});
+          }
+        } else {
+          // A later token's value must not reach a row, not even times zero: token by token.
+          for (int y = 0; y < parts; ++y) {
+#pragma unroll 1
+            for (int j = 0; j < C; ++j) {
+              const bool second = j >= 16;
+              u32x4 one, pj;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t v = y ? (second ? vo[1][1][i] : vo[1][0][i]) : (second ? vo[0][1][i] : vo[0][0][i]);
+                const bool mine = h == ((j >> 2) & 1) && i == 2 * ((j >> 3) & 1) + ((j >> 1) & 1);
+                one[i] = mine ? v & ((j & 1) ? 0xffff0000u : 0xffffu) : 0u;
+                pj[i] = second ? pp[4 + i] : pp[i];
+              }
+              f32x16 with = o;
+              Tile<MAFAT_BF16>::mul(with, one, pj);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[r] = j <= c ? with[r] : o[r];
+            }
+          }
+        }
+        // Row c's outputs: halves of the wave exchange groups of 4, so that each has 8 in a row.
+        const float by = steep ? a.scale : a.scale * e_here;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t w[2][2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) w[x][y] = pack_bf16(o[8 * i + 4 * x + 2 * y] * by, o[8 * i + 4 * x + 2 * y + 1] * by);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const auto two = __builtin_amdgcn_permlane32_swap(w[0][y], w[1][y], false, false);
+            done[i][y] = two[0];
+            done[i][2 + y] = two[1];
+          }
+        }
+        done_at = c < n ? static_cast<uint16_t*>(a.y) + (seg.first + static_cast<int64_t>(t) * C + c) * a.y_row +
+                              (kv * a.group + g) * a.y_head + c0 + 32 * wave + 8 * h
+                        : nullptr;
+      }
+      if (g + 1 < heads) continue;
+      // the state after the chunk
+      if (steep) times(all);
+      else lag += all;
+#pragma unroll
+      for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const s16x4 two[2] = {
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (k_lo ^ (x << 6)) + k_half + 16 * u * KPITCH)),
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (k_hi ^ (x << 6)) + k_half + 16 * u * KPITCH))};
+          const u32x4 kf = __builtin_bit_cast(u32x4, two);
+#pragma unroll
+          for (int y = 0; y < 3; ++y) Tile<MAFAT_BF16>::mul(s[x], kf, vp3[y][u]);
+        }
+    }
+  }
+  times(lag);
+  if constexpr (OUT) write_done();
+  float* const to = !OUT ? part : seg.index + 1 == seg.count ? kept : nullptr;
+  if (to) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = dk_of(t, r, h);
+        if (row < a.key_dim && col < a.value_dim) to[static_cast<int64_t>(row) * a.value_dim + col] = s[t][r];
+      }
+  }
+  if (!OUT && slice == 0 && threadIdx.x == 0)
+    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
+}
+
+template <int KP, int NW, int MODE>
+hipError_t launch(DecayArgs a, hipStream_t stream) {
+  a.slices = (a.value_dim + 32 * NW - 1) / (32 * NW);
+  return for_decay_blocks(a, [&](const DecayArgs& p, unsigned n) {
+    hipLaunchKernelGGL((decay_chunk_kernel<KP, NW, MODE>), dim3(n), dim3(64 * NW), 0, stream, p);
+  });
+}
+
+template <int MODE>
+hipError_t launch_mode(const DecayArgs& a, hipStream_t stream) {
+  const bool few = a.value_dim <= 64;
+  if (a.key_dim <= 64) return few ? launch<64, 2, MODE>(a, stream) : launch<64, 4, MODE>(a, stream);
+  if (a.key_dim <= 128) return few ? launch<128, 2, MODE>(a, stream) : launch<128, 4, MODE>(a, stream);
+  return few ? launch<256, 2, MODE>(a, stream) : launch<256, 4, MODE>(a, stream);
+}
+
+}  // namespace
+
+bool decay_bf16_fits(const DecayArgs& a) {
+  const auto whole = [](const void* p, int64_t row, int64_t head) {
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (row | head))) & 15) == 0 && row < (1 << 25);
+  };
+  return a.key_dim % 8 == 0 && a.value_dim % 8 == 0 && whole(a.q, a.q_row, a.q_head) && whole(a.k, a.k_row, a.k_head) &&
+         whole(a.v, a.v_row, a.v_head);
+}
+
+hipError_t launch_decay_bf16(int mode, const DecayArgs& a, hipStream_t stream) {
+  return mode == DECAY_ADDS ? launch_mode<DECAY_ADDS>(a, stream) : launch_mode<DECAY_OUTPUTS>(a, stream);
+}
+
+}  // namespace mafat
