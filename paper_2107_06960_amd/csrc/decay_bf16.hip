@@ -128,6 +128,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
   constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH;
   constexpr bool OUT = MODE == DECAY_OUTPUTS;
+  constexpr int AHEAD = 4, TAHEAD = KT < 4 ? KT : 4;  // steps and tiles whose fragments are asked for at once
   __shared__ __align__(1024) unsigned char smem[2 * (KTILE + VTILE + (OUT ? KTILE : 0))];
   __shared__ __align__(16) float table[NW][2][C];  // of each wave: c_j, and the values' weights
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
@@ -256,6 +257,23 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         if constexpr (OUT) issue_q(t + 1, 0, at + 1);
       }
       const unsigned char* k = sk + (t & 1) * KTILE;
+      // (Addresses from these are formed here every time: kept over the loop they
+      // would take the registers that hold fragments.)
+      int row_here = row_at, lo_here = k_lo, hi_here = k_hi, table_here = 4 * h;
+      asm volatile("" : "+v"(row_here), "+v"(lo_here), "+v"(hi_here), "+v"(table_here));
+      // The fragments of AHEAD steps are asked for at once (the compiler by itself asks
+      // for a step's fragments just ahead of it).
+      u32x4 qf[OUT ? AHEAD : 1], kf[OUT ? AHEAD : 1];
+      const unsigned char* q = sq + (at & 1) * KTILE;
+      auto fragment = [&](int x) {
+        qf[x % AHEAD] = *reinterpret_cast<const u32x4*>(q + (row_here ^ (x << 5)));
+        kf[x % AHEAD] = *reinterpret_cast<const u32x4*>(k + (row_here ^ (x << 5)));
+      };
+      if constexpr (OUT) {
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) fragment(x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       if (g == 0) {
         if (more) ask_decay(t + 1);
         const double step = c < n || !a.decay_by_row ? static_cast<double>(decay_log2(decay)) : 0.0;
@@ -291,33 +309,43 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
       }
       f32x16 p, o;
       if constexpr (OUT) {
-        const unsigned char* q = sq + (at & 1) * KTILE;
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[i] = o[i] = 0.f;
 #pragma unroll
         for (int x = 0; x < STEPS; ++x) {
-          const u32x4 qf = *reinterpret_cast<const u32x4*>(q + (row_at ^ (x << 5)));
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(k + (row_at ^ (x << 5)));
-          u32x4 sp[2];
+          u32x4 sf;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t two[2];
-            split(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1], two);
-            sp[0][i] = two[0];
-            sp[1][i] = two[1];
+          for (int i = 0; i < 4; ++i) sf[i] = pack_bf16(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1]);
+          Tile<MAFAT_BF16>::mul(p, kf[x % AHEAD], qf[x % AHEAD]);
+          Tile<MAFAT_BF16>::mul(o, sf, qf[x % AHEAD]);
+          if (x + AHEAD < STEPS) {
+            fragment(x + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
           }
-          Tile<MAFAT_BF16>::mul(p, kf, qf);
-          Tile<MAFAT_BF16>::mul(o, sp[0], qf);
-          Tile<MAFAT_BF16>::mul(o, sp[1], qf);
         }
       }
+      // the keys' transposed fragments of the first tiles, likewise
+      u32x4 tf[TAHEAD][2];
+      auto turned = [&](int first) {
+#pragma unroll
+        for (int x = 0; x < TAHEAD; ++x)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const s16x4 two[2] = {
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (lo_here ^ ((first + x) << 6)) + k_half + 16 * u * KPITCH)),
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (hi_here ^ ((first + x) << 6)) + k_half + 16 * u * KPITCH))};
+            tf[x][u] = __builtin_bit_cast(u32x4, two);
+          }
+      };
+      if (g + 1 == heads) turned(0);
+      __builtin_amdgcn_sched_barrier(0);
       // the values, weighted
       u32x4 vp3[3][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const f32x4 w = *reinterpret_cast<const f32x4*>(tw + 16 * u + 8 * i + 4 * h);
+          const f32x4 w = *reinterpret_cast<const f32x4*>(tw + 16 * u + 8 * i + table_here);
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             uint32_t part3[3];
@@ -326,14 +354,14 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
             for (int y = 0; y < 3; ++y) vp3[y][u][2 * i + x] = part3[y];
           }
         }
+      u32x4 p0, p1;  // scores, masked
       if constexpr (OUT) {
-        uint32_t pp[8];
         if (steep) {
           // c_i and c_j as float32: off by 2^-24 of their size, at most 6400, far
           // below the scores' rounding
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + 4 * h);
+            const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + table_here);
 #pragma unroll
             for (int x = 0; x < 4; ++x) p[4 * i + x] *= __builtin_amdgcn_exp2f(c_here - cj[x]);
           }
@@ -341,40 +369,58 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
           for (int i = 0; i < 16; ++i) o[i] *= e_here;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pp[i] = pack_bf16(p[2 * i], p[2 * i + 1]) & below[i];
-        // Values of one part as they are, or weighted ones in two.
-        const int parts = steep ? 1 : 2;
-        u32x4 vo[2][2] = {{vf[0], vf[1]}, {vp3[1][0], vp3[1][1]}};
-        if (!steep) {
-          vo[0][0] = vp3[0][0];
-          vo[0][1] = vp3[0][1];
+        for (int i = 0; i < 4; ++i) {
+          p0[i] = pack_bf16(p[2 * i], p[2 * i + 1]) & below[i];
+          p1[i] = pack_bf16(p[8 + 2 * i], p[8 + 2 * i + 1]) & below[4 + i];
+        }
+      }
+      if (g + 1 == heads) {  // the state after the chunk
+        if (steep) times(all);
+        else lag += all;
+#pragma unroll
+        for (int x0 = 0; x0 < KT; x0 += TAHEAD) {
+          if (x0) turned(x0);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int y = 0; y < 3; ++y)
+#pragma unroll
+              for (int x = 0; x < TAHEAD; ++x) Tile<MAFAT_BF16>::mul(s[x0 + x], tf[x][u], vp3[y][u]);
+        }
+      }
+      if constexpr (OUT) {
+        // The chunk's own part: weighted values in two parts, or values as they are.
+        if (steep) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            vp3[0][u] = vf[u];
+            vp3[1][u] = u32x4{0, 0, 0, 0};
+          }
         }
         if (!odd) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u) Tile<MAFAT_BF16>::mul(o, vo[0][u], u32x4{pp[4 * u], pp[4 * u + 1], pp[4 * u + 2], pp[4 * u + 3]});
-          if (!steep) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) Tile<MAFAT_BF16>::mul(o, vo[1][u], u32x4{pp[4 * u], pp[4 * u + 1], pp[4 * u + 2], pp[4 * u + 3]});
+          for (int y = 0; y < 2; ++y) {
+            Tile<MAFAT_BF16>::mul(o, vp3[y][0], p0);
+            Tile<MAFAT_BF16>::mul(o, vp3[y][1], p1);
           }
         } else {
           // A later token's value must not reach a row, not even times zero: token by token.
-          for (int y = 0; y < parts; ++y) {
 #pragma unroll 1
-            for (int j = 0; j < C; ++j) {
-              const bool second = j >= 16;
-              u32x4 one, pj;
+          for (int j = 0; j < 2 * C; ++j) {
+            const bool second = j & 16, low = j >= C;
+            const int token = j & (C - 1);
+            u32x4 one, pj;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t v = y ? (second ? vo[1][1][i] : vo[1][0][i]) : (second ? vo[0][1][i] : vo[0][0][i]);
-                const bool mine = h == ((j >> 2) & 1) && i == 2 * ((j >> 3) & 1) + ((j >> 1) & 1);
-                one[i] = mine ? v & ((j & 1) ? 0xffff0000u : 0xffffu) : 0u;
-                pj[i] = second ? pp[4 + i] : pp[i];
-              }
-              f32x16 with = o;
-              Tile<MAFAT_BF16>::mul(with, one, pj);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[r] = j <= c ? with[r] : o[r];
+            for (int i = 0; i < 4; ++i) {
+              const bool mine = h == ((j >> 2) & 1) && i == 2 * ((j >> 3) & 1) + ((j >> 1) & 1);
+              const uint32_t v = low ? (second ? vp3[1][1][i] : vp3[1][0][i]) : (second ? vp3[0][1][i] : vp3[0][0][i]);
+              one[i] = mine ? v & ((j & 1) ? 0xffff0000u : 0xffffu) : 0u;
+              pj[i] = second ? p1[i] : p0[i];
             }
+            f32x16 with = o;
+            Tile<MAFAT_BF16>::mul(with, one, pj);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[r] = token <= c ? with[r] : o[r];
           }
         }
         // Row c's outputs: halves of the wave exchange groups of 4, so that each has 8 in a row.
@@ -397,21 +443,6 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
                               (kv * a.group + g) * a.y_head + c0 + 32 * wave + 8 * h
                         : nullptr;
       }
-      if (g + 1 < heads) continue;
-      // the state after the chunk
-      if (steep) times(all);
-      else lag += all;
-#pragma unroll
-      for (int x = 0; x < KT; ++x)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const s16x4 two[2] = {
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (k_lo ^ (x << 6)) + k_half + 16 * u * KPITCH)),
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(k + (k_hi ^ (x << 6)) + k_half + 16 * u * KPITCH))};
-          const u32x4 kf = __builtin_bit_cast(u32x4, two);
-#pragma unroll
-          for (int y = 0; y < 3; ++y) Tile<MAFAT_BF16>::mul(s[x], kf, vp3[y][u]);
-        }
     }
   }
   times(lag);
