@@ -120,9 +120,11 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   __shared__ int odd;  // whether the chunk's values are not all finite
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int l16 = lane & 15, h4 = lane >> 4;
-  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.blocks);
-  const int bh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.slices));
-  const int slice = id - bh * a.slices;
+  // (Slices last: workgroups go round the XCDs, and segments that are not there come
+  // last, so that every XCD has as many that are.)
+  const int id = a.first_block + static_cast<int>(blockIdx.x), all_bh = a.segments * a.kv_heads;
+  const int slice = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(all_bh));
+  const int bh = id - slice * all_bh;
   const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = bh - b * a.kv_heads;
   const Segment seg = find_segment(a, b);
@@ -282,30 +284,32 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 }
 
 // What segments add -> what they start from, for requests of several segments.
-// A thread takes one entry of a head's state through the segments.
+// A thread takes V entries of a head's state through the segments, with the next
+// kJoinAhead of them on their way.
 constexpr int kJoinAhead = 8;
+template <int V>
 __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
+  typedef float fv __attribute__((ext_vector_type(V)));
   const int64_t size = static_cast<int64_t>(a.key_dim) * a.value_dim;
-  const int per = static_cast<int>((size + 255) / 256);
+  const int per = static_cast<int>((size + 256 * V - 1) / (256 * V));
   const int id = a.first_block + static_cast<int>(blockIdx.x);
   const int rh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(per));
-  const int64_t e = static_cast<int64_t>(id - rh * per) * 256 + threadIdx.x;
+  const int64_t e = V * (static_cast<int64_t>(id - rh * per) * 256 + threadIdx.x);
   const int request = static_cast<int>(static_cast<uint32_t>(rh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = rh - request * a.kv_heads;
   // the request's first segment, and how many there are
-  const uint32_t len = static_cast<uint32_t>(a.segment);
-  int first, n;
+  int first, n, length;
   rows_of(a, request, &first, &n);
-  const int count = static_cast<int>((static_cast<uint32_t>(n) + len - 1) / len);
+  const int count = segments_of(a, n, &length);
   if (count < 2) return;
   uint32_t b = static_cast<uint32_t>(request) * static_cast<uint32_t>(count);
   if (a.offsets) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     b = 0;
     for (int r = lane; r < request; r += 64) {
-      int lo, m;
+      int lo, m, len;
       rows_of(a, r, &lo, &m);
-      b += (static_cast<uint32_t>(m) + len - 1) / len;
+      b += static_cast<uint32_t>(segments_of(a, m, &len));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) b += static_cast<uint32_t>(__shfl_xor(static_cast<int>(b), o, 64));
@@ -313,23 +317,32 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   if (b + static_cast<uint32_t>(count) > static_cast<uint32_t>(a.segments)) return;  // (offsets that decrease)
   const int64_t slot = slot_of(a, request);
   if (e >= size) return;
-  float s = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
-  if (slot >= 0) s = a.states[slot * a.state_slot + kv * size + e];
+  const float start = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
+  fv s;
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = start;
+  if (slot >= 0) __builtin_memcpy(&s, a.states + slot * a.state_slot + kv * size + e, sizeof(s));
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * size + e;
   const float* const factor = a.factor + static_cast<int64_t>(b) * a.kv_heads + kv;
   const int64_t step = a.kv_heads * size;
   for (int i0 = 0; i0 < count; i0 += kJoinAhead) {
-    float adds[kJoinAhead], by[kJoinAhead];
+    fv adds[kJoinAhead];
+    float by[kJoinAhead];
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i) {
-      const bool there = i0 + i + 1 < count;  // (the last adds nothing to another's start)
-      adds[i] = there ? part[(i0 + i) * step] : 0.f;
-      by[i] = there ? factor[static_cast<int64_t>(i0 + i) * a.kv_heads] : 0.f;
+      by[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) adds[i][j] = 0.f;
+      if (i0 + i + 1 < count) {  // (the last adds nothing to another's start)
+        __builtin_memcpy(&adds[i], part + (i0 + i) * step, sizeof(s));
+        by[i] = factor[static_cast<int64_t>(i0 + i) * a.kv_heads];
+      }
     }
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i) {
-      if (i0 + i < count) part[(i0 + i) * step] = s;
-      s = fmaf(s, by[i], adds[i]);
+      if (i0 + i < count) __builtin_memcpy(part + (i0 + i) * step, &s, sizeof(s));
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] = fmaf(s[j], by[i], adds[i][j]);
     }
   }
 }
@@ -345,12 +358,14 @@ hipError_t launch_chunks(DecayArgs a, hipStream_t stream) {
   });
 }
 
+template <int V>
 hipError_t launch_join(DecayArgs a, hipStream_t stream) {
-  const int64_t blocks = static_cast<int64_t>(a.requests) * a.kv_heads * ((static_cast<int64_t>(a.key_dim) * a.value_dim + 255) / 256);
+  const int64_t size = static_cast<int64_t>(a.key_dim) * a.value_dim;
+  const int64_t blocks = static_cast<int64_t>(a.requests) * a.kv_heads * ((size + 256 * V - 1) / (256 * V));
   if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
   return for_block_parts(blocks, [&](int32_t from, unsigned n) {
     a.first_block = from;
-    hipLaunchKernelGGL(decay_join_kernel, dim3(n), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decay_join_kernel<V>), dim3(n), dim3(256), 0, stream, a);
   });
 }
 
@@ -373,7 +388,8 @@ hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
   // (without offsets the requests' lengths are known)
   if (p.split && (a.offsets || a.per_request > a.segment)) {
     hipError_t e = launch_chunks<DT, DECAY_ADDS>(a, stream);
-    if (e == hipSuccess) e = launch_join(a, stream);
+    // (entries four at a time where states are whole fours)
+    if (e == hipSuccess) e = a.key_dim * a.value_dim % 4 == 0 ? launch_join<4>(a, stream) : launch_join<1>(a, stream);
     if (e != hipSuccess) return e;
   }
   return launch_chunks<DT, DECAY_OUTPUTS>(a, stream);

@@ -73,6 +73,19 @@ struct TileFetch {
   }
 };
 
+// As load_to_lds, 4 bytes a lane.
+__device__ __forceinline__ void load4_to_lds(const u32x4& range, unsigned off, unsigned to) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(range[i])));
+  to = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(to), "v"(off), "s"(r)
+               : "memory");
+}
+
 // Entry of the keys that register r of tile t holds in lanes of half h.
 __device__ __forceinline__ int dk_of(int t, int r, int h) { return 32 * t + 16 * (r >> 3) + 8 * h + (r & 7); }
 
@@ -123,19 +136,24 @@ __device__ __forceinline__ double scan32(double v, double* all) {
   return v;
 }
 
+// Chunks are asked for SLOTS - 1 iterations ahead, an iteration being a chunk and
+// a query head of the group: the memory's answer takes longer than one.
 template <int KP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
-  constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH;
   constexpr bool OUT = MODE == DECAY_OUTPUTS;
+  constexpr int SLOTS = OUT ? 3 : 4;
+  constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH, DTILE = NW * 256;
   constexpr int AHEAD = 4, TAHEAD = KT < 4 ? KT : 4;  // steps and tiles whose fragments are asked for at once
-  __shared__ __align__(1024) unsigned char smem[2 * (KTILE + VTILE + (OUT ? KTILE : 0))];
+  __shared__ __align__(1024) unsigned char smem[SLOTS * (KTILE + VTILE + DTILE + (OUT ? KTILE : 0))];
   __shared__ __align__(16) float table[NW][2][C];  // of each wave: c_j, and the values' weights
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int id = xcd_remap(a.first_block + static_cast<int>(blockIdx.x), a.blocks);
-  const int bh = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(a.slices));
-  const int slice = id - bh * a.slices;
+  // (Slices last: workgroups go round the XCDs, and segments that are not there come
+  // last, so that every XCD has as many that are.)
+  const int id = a.first_block + static_cast<int>(blockIdx.x), all_bh = a.segments * a.kv_heads;
+  const int slice = static_cast<int>(static_cast<uint32_t>(id) / static_cast<uint32_t>(all_bh));
+  const int bh = id - slice * all_bh;
   const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = bh - b * a.kv_heads;
   const Segment seg = find_segment(a, b);
@@ -144,48 +162,61 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   const int c0 = 32 * NW * slice, col = c0 + 32 * wave + c;  // of the state
   const int chunks = (seg.n + C - 1) / C;
   unsigned char* const sk = smem;
-  unsigned char* const sv = smem + 2 * KTILE;
-  unsigned char* const sq = smem + 2 * (KTILE + VTILE);
+  unsigned char* const sv = sk + SLOTS * KTILE;
+  unsigned char* const sd = sv + SLOTS * VTILE;  // the tokens' decays, for each wave
+  unsigned char* const sq = sd + SLOTS * DTILE;
   TileFetch<KPITCH, NW> fk, fq;
   TileFetch<VPITCH, NW> fv;
+  constexpr int LOADS_Q = OUT ? TileFetch<KPITCH, NW>::LOADS : 0;
+  constexpr int LOADS_KV = TileFetch<KPITCH, NW>::LOADS + TileFetch<VPITCH, NW>::LOADS + 1;
+  static_assert(2 * (LOADS_Q + LOADS_KV) <= 63, "loads in flight that a wave can count");
   fk.start(a.k, seg.first * a.k_row + kv * a.k_head, a.k_row, a.key_dim, wave);
   fv.start(a.v, seg.first * a.v_row + kv * a.v_head + c0, a.v_row, a.value_dim - c0, wave);
+  if constexpr (OUT) fq.start(a.q, 0, a.q_row, a.key_dim, wave);
+  const int d_row = a.decay_by_row ? static_cast<int>(a.decay_row) : 0;  // (all tokens read the head's one)
   const float* const decays = a.log_decay + (a.decay_by_row ? seg.first * a.decay_row : 0) + kv;
-  auto issue_kv = [&](int t) {
-    const int n = min(C, seg.n - t * C);
-    fk.issue(static_cast<int64_t>(t) * C, n, lds_offset(sk) + (t & 1) * KTILE, wave);
-    fv.issue(static_cast<int64_t>(t) * C, n, lds_offset(sv) + (t & 1) * VTILE, wave);
+  const int heads = OUT ? a.group : 1;
+  // The iteration that is asked for next, and its slots.
+  int ask_t = 0, ask_g = 0, ask_kv = 0, ask_q = 0;
+  auto ask = [&] {
+    const int n = min(C, seg.n - ask_t * C);
+    const int64_t row0 = static_cast<int64_t>(ask_t) * C;
+    if (ask_g == 0) {
+      fk.issue(row0, n, lds_offset(sk) + ask_kv * KTILE, wave);
+      fv.issue(row0, n, lds_offset(sv) + ask_kv * VTILE, wave);
+      load4_to_lds(range_of(decays + row0 * d_row, static_cast<unsigned>(4 * ((n - 1) * d_row + 1))),
+                   static_cast<unsigned>(4 * c * d_row), lds_offset(sd) + ask_kv * DTILE + wave * 256);
+      ask_kv = ask_kv + 1 == SLOTS ? 0 : ask_kv + 1;
+    }
+    if constexpr (OUT) {
+      fq.base = static_cast<const uint16_t*>(a.q) + seg.first * a.q_row + (kv * a.group + ask_g) * a.q_head;
+      fq.issue(row0, n, lds_offset(sq) + ask_q * KTILE, wave);
+      ask_q = ask_q + 1 == SLOTS ? 0 : ask_q + 1;
+    }
+    ask_g = ask_g + 1 == heads ? 0 : ask_g + 1;
+    ask_t += ask_g == 0 ? 1 : 0;
   };
-  // Head g of the group, chunk t; `at` counts both.
-  auto issue_q = [&](int t, int g, int at) {
-    fq.base = static_cast<const uint16_t*>(a.q) + seg.first * a.q_row + (kv * a.group + g) * a.q_head;
-    fq.issue(static_cast<int64_t>(t) * C, min(C, seg.n - t * C), lds_offset(sq) + (at & 1) * KTILE, wave);
-  };
-  issue_kv(0);
-  if constexpr (OUT) {
-    fq.start(a.q, 0, a.q_row, a.key_dim, wave);
-    issue_q(0, 0, 0);
-  }
-  float next_decay = 0.f;  // of token c of the next chunk
-  auto ask_decay = [&](int t) {
-    const int i = t * C + c;
-    next_decay = i < seg.n ? decays[a.decay_by_row ? i * a.decay_row : 0] : 0.f;
-  };
-  ask_decay(0);
+#pragma unroll
+  for (int i = 0; i < SLOTS - 1; ++i)
+    if (ask_t < chunks) ask();
 
   const int64_t slot = OUT && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
   float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
+  // The state's entries by a descriptor: what is past its rows or columns reads as
+  // zero and is not written, without a branch for each.
+  const unsigned state_bytes = static_cast<unsigned>(4 * a.key_dim * a.value_dim);
+  auto entry = [&](int t, int r) {
+    return col < a.value_dim ? static_cast<unsigned>(4 * (dk_of(t, r, h) * a.value_dim + col)) : 0x80000000u;
+  };
   f32x16 s[KT];
   if (OUT && (kept || seg.count > 1)) {
-    const float* from = seg.count > 1 ? part : kept;
+    const auto from = make_rsrc(seg.count > 1 ? part : kept, state_bytes);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = dk_of(t, r, h);
-        s[t][r] = row < a.key_dim && col < a.value_dim ? from[static_cast<int64_t>(row) * a.value_dim + col] : 0.f;
-      }
+      for (int r = 0; r < 16; ++r)
+        s[t][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, static_cast<int>(entry(t, r)), 0, 0));
   } else {
     const float f = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
 #pragma unroll
@@ -215,7 +246,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
 
   wait_loads();
   double total = 0.0, lag = 0.0;  // of the segment's decays, in base 2; A
-  int at = 0;          // chunks and heads so far
+  int kv_slot = 0, q_slot = 0;
   u32x4 done[2] = {};  // outputs of the last chunk, still to be written
   uint16_t* done_at = nullptr;
   auto write_done = [&] {
@@ -239,24 +270,20 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
     bool steep = false;                     // exponentials of differences
     u32x4 vf[2];
     bool odd = false;
-    const int heads = OUT ? a.group : 1;
-    for (int g = 0; g < heads; ++g, ++at) {
-      // Everything asked for an iteration ago is there, and its outputs are written.
-      wait_loads();
-      wg_barrier_writes();  // for all waves, and nobody reads the other slots any more
-      // (The compiler waits for the decay where it is first used, and knows
-      // nothing of the loads into LDS: before they are asked for.)
-      float decay = next_decay;
-      asm volatile("" : "+v"(decay));
-      if constexpr (OUT) write_done();
-      const bool more = t + 1 < chunks;
-      if (g + 1 < heads) {
-        issue_q(t, g + 1, at + 1);
-      } else if (more) {
-        issue_kv(t + 1);
-        if constexpr (OUT) issue_q(t + 1, 0, at + 1);
+    for (int g = 0; g < heads; ++g) {
+      // What this iteration reads is there; what was asked for after it may be on its way
+      // (loads complete in order, and stores in between only make the wait longer).
+      if constexpr (OUT) {
+        if (g + 1 < heads) wait_vmcnt<LOADS_Q>();
+        else if (t + 1 < chunks) wait_vmcnt<LOADS_Q + LOADS_KV>();
+        else wait_vmcnt<0>();
+      } else {
+        wait_stage<LOADS_KV, SLOTS - 2>(chunks - 1 - t);
       }
-      const unsigned char* k = sk + (t & 1) * KTILE;
+      wg_barrier_writes();  // for all waves, and nobody reads the slots that are asked for next any more
+      if constexpr (OUT) write_done();
+      if (ask_t < chunks) ask();
+      const unsigned char* k = sk + kv_slot * KTILE;
       // (Addresses from these are formed here every time: kept over the loop they
       // would take the registers that hold fragments.)
       int row_here = row_at, lo_here = k_lo, hi_here = k_hi, table_here = 4 * h;
@@ -264,7 +291,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
       // The fragments of AHEAD steps are asked for at once (the compiler by itself asks
       // for a step's fragments just ahead of it).
       u32x4 qf[OUT ? AHEAD : 1], kf[OUT ? AHEAD : 1];
-      const unsigned char* q = sq + (at & 1) * KTILE;
+      const unsigned char* q = sq + q_slot * KTILE;
       auto fragment = [&](int x) {
         qf[x % AHEAD] = *reinterpret_cast<const u32x4*>(q + (row_here ^ (x << 5)));
         kf[x % AHEAD] = *reinterpret_cast<const u32x4*>(k + (row_here ^ (x << 5)));
@@ -275,8 +302,8 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         __builtin_amdgcn_sched_barrier(0);
       }
       if (g == 0) {
-        if (more) ask_decay(t + 1);
-        const double step = c < n || !a.decay_by_row ? static_cast<double>(decay_log2(decay)) : 0.0;
+        const float decay = *reinterpret_cast<const float*>(sd + kv_slot * DTILE + wave * 256 + 4 * lane);
+        const double step = decay_log2(decay);  // (0 of tokens that are not there)
         double ci;
         if (a.decay_by_row) {
           ci = scan32(step, &all);
@@ -295,7 +322,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         e_here = __builtin_amdgcn_exp2f(static_cast<float>(lag + ci));
         tc[c] = c_here;
         tw[c] = __builtin_amdgcn_exp2f(static_cast<float>(steep ? all - ci : -lag - ci));
-        const unsigned char* v = sv + (t & 1) * VTILE;
+        const unsigned char* v = sv + kv_slot * VTILE;
         uint32_t bad = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -442,20 +469,21 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         done_at = c < n ? static_cast<uint16_t*>(a.y) + (seg.first + static_cast<int64_t>(t) * C + c) * a.y_row +
                               (kv * a.group + g) * a.y_head + c0 + 32 * wave + 8 * h
                         : nullptr;
+        q_slot = q_slot + 1 == SLOTS ? 0 : q_slot + 1;
       }
     }
+    kv_slot = kv_slot + 1 == SLOTS ? 0 : kv_slot + 1;
   }
   times(lag);
   if constexpr (OUT) write_done();
   float* const to = !OUT ? part : seg.index + 1 == seg.count ? kept : nullptr;
   if (to) {
+    const auto rsrc = make_rsrc(to, state_bytes);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = dk_of(t, r, h);
-        if (row < a.key_dim && col < a.value_dim) to[static_cast<int64_t>(row) * a.value_dim + col] = s[t][r];
-      }
+      for (int r = 0; r < 16; ++r)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[t][r]), rsrc, static_cast<int>(entry(t, r)), 0, 0);
   }
   if (!OUT && slice == 0 && threadIdx.x == 0)
     a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
@@ -484,7 +512,7 @@ bool decay_bf16_fits(const DecayArgs& a) {
     return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (row | head))) & 15) == 0 && row < (1 << 25);
   };
   return a.key_dim % 8 == 0 && a.value_dim % 8 == 0 && whole(a.q, a.q_row, a.q_head) && whole(a.k, a.k_row, a.k_head) &&
-         whole(a.v, a.v_row, a.v_head);
+         whole(a.v, a.v_row, a.v_head) && (!a.decay_by_row || a.decay_row < (1 << 24));
 }
 
 hipError_t launch_decay_bf16(int mode, const DecayArgs& a, hipStream_t stream) {

@@ -53,6 +53,20 @@ __device__ __forceinline__ int64_t slot_of(const DecayArgs& a, int request) {
   return s;
 }
 
+// The segments of a request of n rows, and their length: as few as a segment's
+// largest length allows, as even as whole chunks of 32 tokens go.
+__device__ __forceinline__ int segments_of(const DecayArgs& a, int n, int* length) {
+  const uint32_t rows = static_cast<uint32_t>(n), most = static_cast<uint32_t>(a.segment);
+  if (rows <= most) {
+    *length = a.segment;
+    return rows > 0 ? 1 : 0;
+  }
+  const uint32_t count = (rows + most - 1) / most;
+  const uint32_t len = ((rows + count - 1) / count + 31) & ~31u;
+  *length = static_cast<int>(len);
+  return static_cast<int>((rows + len - 1) / len);
+}
+
 // A block's work: a segment of a request.
 struct Segment {
   int request, first, n;  // rows of the segment
@@ -65,11 +79,10 @@ struct Segment {
 __device__ __forceinline__ Segment find_segment(const DecayArgs& a, int b) {
   Segment s;
   s.any = true;
-  const uint32_t len = static_cast<uint32_t>(a.segment);
-  int start, rows;
+  int start, rows, length;
   if (!a.offsets) {
     rows = a.per_request;
-    s.count = static_cast<int>((static_cast<uint32_t>(rows) + len - 1) / len);
+    s.count = segments_of(a, rows, &length);
     s.request = static_cast<int>(static_cast<uint32_t>(b) / static_cast<uint32_t>(s.count));
     s.index = b - s.request * s.count;
     start = s.request * rows;
@@ -78,12 +91,12 @@ __device__ __forceinline__ Segment find_segment(const DecayArgs& a, int b) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     uint32_t before = 0;
     s.any = false;
-    s.request = s.index = s.count = start = rows = 0;
+    s.request = s.index = s.count = start = rows = length = 0;
     for (int r0 = 0; r0 < a.requests; r0 += 64) {
       const int r = r0 + lane;
-      int lo = 0, n = 0;
+      int lo = 0, n = 0, len;
       if (r < a.requests) rows_of(a, r, &lo, &n);
-      const uint32_t blocks = (static_cast<uint32_t>(n) + len - 1) / len;
+      const uint32_t blocks = static_cast<uint32_t>(segments_of(a, n, &len));
       // (offsets that decrease may make the sums wrap: b then matches some request or none)
       uint32_t upto = blocks;
 #pragma unroll
@@ -98,6 +111,7 @@ __device__ __forceinline__ Segment find_segment(const DecayArgs& a, int b) {
         s.request = r0 + l;
         start = __builtin_amdgcn_readlane(lo, l);
         rows = __builtin_amdgcn_readlane(n, l);
+        length = __builtin_amdgcn_readlane(len, l);
         s.index = __builtin_amdgcn_readlane(static_cast<int>(mine), l);
         s.count = __builtin_amdgcn_readlane(static_cast<int>(blocks), l);
         s.any = true;
@@ -106,8 +120,8 @@ __device__ __forceinline__ Segment find_segment(const DecayArgs& a, int b) {
       before += static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(upto), 63));
     }
   }
-  s.first = start + s.index * a.segment;
-  s.n = min(a.segment, rows - s.index * a.segment);
+  s.first = start + s.index * length;
+  s.n = min(length, rows - s.index * length);
   return s;
 }
 
