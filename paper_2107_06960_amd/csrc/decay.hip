@@ -285,9 +285,8 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 
 // What segments add -> what they start from, for requests of several segments.
 // A thread takes V entries of a head's state through the segments, with the next
-// kJoinAhead of them on their way.
-constexpr int kJoinAhead = 8;
-template <int V>
+// AHEAD of them on their way.
+template <int V, int AHEAD>
 __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   typedef float fv __attribute__((ext_vector_type(V)));
   const int64_t size = static_cast<int64_t>(a.key_dim) * a.value_dim;
@@ -325,11 +324,11 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * size + e;
   const float* const factor = a.factor + static_cast<int64_t>(b) * a.kv_heads + kv;
   const int64_t step = a.kv_heads * size;
-  for (int i0 = 0; i0 < count; i0 += kJoinAhead) {
-    fv adds[kJoinAhead];
-    float by[kJoinAhead];
+  for (int i0 = 0; i0 < count; i0 += AHEAD) {
+    fv adds[AHEAD];
+    float by[AHEAD];
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
+    for (int i = 0; i < AHEAD; ++i) {
       by[i] = 0.f;
 #pragma unroll
       for (int j = 0; j < V; ++j) adds[i][j] = 0.f;
@@ -339,7 +338,7 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
+    for (int i = 0; i < AHEAD; ++i) {
       if (i0 + i < count) __builtin_memcpy(part + (i0 + i) * step, &s, sizeof(s));
 #pragma unroll
       for (int j = 0; j < V; ++j) s[j] = fmaf(s[j], by[i], adds[i][j]);
@@ -358,14 +357,14 @@ hipError_t launch_chunks(DecayArgs a, hipStream_t stream) {
   });
 }
 
-template <int V>
+template <int V, int AHEAD>
 hipError_t launch_join(DecayArgs a, hipStream_t stream) {
   const int64_t size = static_cast<int64_t>(a.key_dim) * a.value_dim;
   const int64_t blocks = static_cast<int64_t>(a.requests) * a.kv_heads * ((size + 256 * V - 1) / (256 * V));
   if (blocks >= (int64_t{1} << 31)) return hipErrorInvalidValue;
   return for_block_parts(blocks, [&](int32_t from, unsigned n) {
     a.first_block = from;
-    hipLaunchKernelGGL((decay_join_kernel<V>), dim3(n), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decay_join_kernel<V, AHEAD>), dim3(n), dim3(256), 0, stream, a);
   });
 }
 
@@ -388,8 +387,11 @@ hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
   // (without offsets the requests' lengths are known)
   if (p.split && (a.offsets || a.per_request > a.segment)) {
     hipError_t e = launch_chunks<DT, DECAY_ADDS>(a, stream);
-    // (entries four at a time where states are whole fours)
-    if (e == hipSuccess) e = a.key_dim * a.value_dim % 4 == 0 ? launch_join<4>(a, stream) : launch_join<1>(a, stream);
+    // Entries four at a time where there are heads for a wave a SIMD; few heads have many
+    // segments each.
+    const bool many = static_cast<int64_t>(a.requests) * a.kv_heads * a.key_dim * a.value_dim >= 4 * 65536;
+    if (e == hipSuccess)
+      e = many && a.key_dim * a.value_dim % 4 == 0 ? launch_join<4, 8>(a, stream) : launch_join<1, 32>(a, stream);
     if (e != hipSuccess) return e;
   }
   return launch_chunks<DT, DECAY_OUTPUTS>(a, stream);

@@ -45,46 +45,72 @@ __device__ __forceinline__ int turn(int r) {
   return PITCH == 128 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
 }
 
-// A tile of C rows straight into LDS: each wave its loads of 1 KB.
+// 16 (or 4) bytes a lane from byte off + `at` of a descriptor's range (zeros past
+// it) straight into LDS, lane after lane from byte `to`; see load_to_lds.  The
+// descriptor stays in scalar registers and `at` moves along, so that a tile takes
+// few instructions.
+__device__ __forceinline__ u32x4 scalar_range(const void* p, unsigned bytes) {
+  const u32x4 v = range_of(p, bytes);
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(v[i])));
+  return r;
+}
+__device__ __forceinline__ void load16_at(const u32x4& r, unsigned off, unsigned at, unsigned to) {
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(to), "v"(off), "s"(r), "s"(at)
+               : "memory");
+}
+__device__ __forceinline__ void load16_at2(const u32x4& r, unsigned off0, unsigned off1, unsigned at, unsigned to0, unsigned to1) {
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %3, %5, %6 offen lds\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(to0), "s"(to1), "v"(off0), "v"(off1), "s"(r), "s"(at)
+               : "memory");
+}
+__device__ __forceinline__ void load4_at(const u32x4& r, unsigned off, unsigned at, unsigned to) {
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dword %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(to), "v"(off), "s"(r), "s"(at)
+               : "memory");
+}
+
+// Tiles of C rows of a segment straight into LDS: each wave its loads of 1 KB.
 template <int PITCH, int NW>
 struct TileFetch {
   static constexpr int PER = PITCH / 16, ROWS = 64 / PER, LOADS = C / ROWS / NW;
   static_assert(LOADS * ROWS * NW == C, "whole loads per wave");
-  const uint16_t* base;
-  int row, dim;
+  u32x4 range;
+  unsigned tile;  // bytes of a tile's rows in memory
   unsigned off[LOADS];
-  __device__ __forceinline__ void start(const void* p, int64_t offset, int64_t stride, int d, int wave) {
-    const int lane = static_cast<int>(threadIdx.x) & 63;
-    base = static_cast<const uint16_t*>(p) + offset;
-    row = static_cast<int>(stride);
-    dim = d;
+  // p: the segment's first row, of n; `stride` elements between rows, `dim` of them
+  // in one.  (The extent is below 2^31 bytes.)
+  __device__ __forceinline__ void start(const uint16_t* p, int n, int64_t stride, int dim, int wave) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, row = static_cast<int>(stride);
+    range = scalar_range(p, static_cast<unsigned>(2 * ((n - 1) * row + dim)));
+    tile = static_cast<unsigned>(2 * C * row);
 #pragma unroll
     for (int g = 0; g < LOADS; ++g) {
       const int r = ROWS * (g * NW + wave) + lane / PER;
       const int at = 8 * ((lane % PER) ^ turn<PITCH>(r));
-      off[g] = at < d ? static_cast<unsigned>(2 * (r * row + at)) : 0x80000000u;
+      off[g] = at < dim ? static_cast<unsigned>(2 * (r * row + at)) : 0x80000000u;
     }
   }
-  // n rows from row0 on (the others read as zeros) to byte `to` of LDS.
-  __device__ __forceinline__ void issue(int64_t row0, int n, unsigned to, int wave) const {
-    const u32x4 range = range_of(base + row0 * row, static_cast<unsigned>(2 * ((n - 1) * row + dim)));
+  // Rows from byte `at` on (those past the segment's last read as zeros) to byte `to` of LDS.
+  __device__ __forceinline__ void issue(unsigned at, unsigned to, int wave) const {
+    constexpr int STEP = ROWS * NW * PITCH;
+    to += ROWS * PITCH * wave;
+    if constexpr (LOADS == 1) {
+      load16_at(range, off[0], at, to);
+    } else {
 #pragma unroll
-    for (int g = 0; g < LOADS; ++g) load_to_lds(range, off[g], to + ROWS * (g * NW + wave) * PITCH);
+      for (int g = 0; g < LOADS; g += 2) load16_at2(range, off[g], off[g + 1], at, to + g * STEP, to + (g + 1) * STEP);
+    }
   }
 };
-
-// As load_to_lds, 4 bytes a lane.
-__device__ __forceinline__ void load4_to_lds(const u32x4& range, unsigned off, unsigned to) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(range[i])));
-  to = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(to)));
-  unsigned m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0)
-               : "s"(to), "v"(off), "s"(r)
-               : "memory");
-}
 
 // Entry of the keys that register r of tile t holds in lanes of half h.
 __device__ __forceinline__ int dk_of(int t, int r, int h) { return 32 * t + 16 * (r >> 3) + 8 * h + (r & 7); }
@@ -170,27 +196,34 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   constexpr int LOADS_Q = OUT ? TileFetch<KPITCH, NW>::LOADS : 0;
   constexpr int LOADS_KV = TileFetch<KPITCH, NW>::LOADS + TileFetch<VPITCH, NW>::LOADS + 1;
   static_assert(2 * (LOADS_Q + LOADS_KV) <= 63, "loads in flight that a wave can count");
-  fk.start(a.k, seg.first * a.k_row + kv * a.k_head, a.k_row, a.key_dim, wave);
-  fv.start(a.v, seg.first * a.v_row + kv * a.v_head + c0, a.v_row, a.value_dim - c0, wave);
-  if constexpr (OUT) fq.start(a.q, 0, a.q_row, a.key_dim, wave);
+  const auto first_row = [&](const void* p, int64_t row, int64_t head) {
+    return static_cast<const uint16_t*>(p) + seg.first * row + head;
+  };
+  fk.start(first_row(a.k, a.k_row, kv * a.k_head), seg.n, a.k_row, a.key_dim, wave);
+  fv.start(first_row(a.v, a.v_row, kv * a.v_head + c0), seg.n, a.v_row, a.value_dim - c0, wave);
+  if constexpr (OUT) fq.start(first_row(a.q, a.q_row, kv * a.group * a.q_head), seg.n, a.q_row, a.key_dim, wave);
   const int d_row = a.decay_by_row ? static_cast<int>(a.decay_row) : 0;  // (all tokens read the head's one)
-  const float* const decays = a.log_decay + (a.decay_by_row ? seg.first * a.decay_row : 0) + kv;
+  const u32x4 decays = scalar_range(a.log_decay + (a.decay_by_row ? seg.first * a.decay_row : 0) + kv,
+                                    static_cast<unsigned>(4 * ((seg.n - 1) * d_row + 1)));
+  const unsigned d_off = static_cast<unsigned>(4 * c * d_row);
   const int heads = OUT ? a.group : 1;
   // The iteration that is asked for next, and its slots.
   int ask_t = 0, ask_g = 0, ask_kv = 0, ask_q = 0;
   auto ask = [&] {
-    const int n = min(C, seg.n - ask_t * C);
-    const int64_t row0 = static_cast<int64_t>(ask_t) * C;
+    const unsigned chunk = static_cast<unsigned>(ask_t);
     if (ask_g == 0) {
-      fk.issue(row0, n, lds_offset(sk) + ask_kv * KTILE, wave);
-      fv.issue(row0, n, lds_offset(sv) + ask_kv * VTILE, wave);
-      load4_to_lds(range_of(decays + row0 * d_row, static_cast<unsigned>(4 * ((n - 1) * d_row + 1))),
-                   static_cast<unsigned>(4 * c * d_row), lds_offset(sd) + ask_kv * DTILE + wave * 256);
+      fk.issue(chunk * fk.tile, lds_offset(sk) + ask_kv * KTILE, wave);
+      fv.issue(chunk * fv.tile, lds_offset(sv) + ask_kv * VTILE, wave);
+      load4_at(decays, d_off, chunk * static_cast<unsigned>(4 * C * d_row), lds_offset(sd) + ask_kv * DTILE + wave * 256);
       ask_kv = ask_kv + 1 == SLOTS ? 0 : ask_kv + 1;
     }
     if constexpr (OUT) {
-      fq.base = static_cast<const uint16_t*>(a.q) + seg.first * a.q_row + (kv * a.group + ask_g) * a.q_head;
-      fq.issue(row0, n, lds_offset(sq) + ask_q * KTILE, wave);
+      if (heads > 1) {
+        const u32x4 base = scalar_range(first_row(a.q, a.q_row, (kv * a.group + ask_g) * a.q_head), 0);
+        fq.range[0] = base[0];
+        fq.range[1] = base[1];
+      }
+      fq.issue(chunk * fq.tile, lds_offset(sq) + ask_q * KTILE, wave);
       ask_q = ask_q + 1 == SLOTS ? 0 : ask_q + 1;
     }
     ask_g = ask_g + 1 == heads ? 0 : ask_g + 1;
@@ -508,11 +541,13 @@ hipError_t launch_mode(const DecayArgs& a, hipStream_t stream) {
 }  // namespace
 
 bool decay_bf16_fits(const DecayArgs& a) {
-  const auto whole = [](const void* p, int64_t row, int64_t head) {
-    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (row | head))) & 15) == 0 && row < (1 << 25);
+  // whole pieces, and a segment's extent in 31 bits
+  const int64_t rows = static_cast<int64_t>(a.segment) + C;
+  const auto whole = [&](const void* p, int64_t row, int64_t head) {
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (row | head))) & 15) == 0 && rows * row < (int64_t{1} << 30) - 512;
   };
   return a.key_dim % 8 == 0 && a.value_dim % 8 == 0 && whole(a.q, a.q_row, a.q_head) && whole(a.k, a.k_row, a.k_head) &&
-         whole(a.v, a.v_row, a.v_head) && (!a.decay_by_row || a.decay_row < (1 << 24));
+         whole(a.v, a.v_row, a.v_head) && (!a.decay_by_row || rows * a.decay_row < (int64_t{1} << 29));
 }
 
 hipError_t launch_decay_bf16(int mode, const DecayArgs& a, hipStream_t stream) {
