@@ -17,7 +17,66 @@
 namespace mafat {
 namespace {
 
-__device__ __forceinline__ float gate_of(float g, int silu) { return (silu ? g : 1.f) / (1.f + expf(-g)); }
+// What every thread of a row forms for itself is kept short, since it has eight
+// values of it: reciprocals and roots are the hardware's, within one unit.
+
+// 1 / sqrt(v); the hardware's root takes denormal numbers for zeros.
+__device__ __forceinline__ float inverse_root(float v) {
+  return v < 0x1p-96f ? 0x1p50f * __builtin_amdgcn_rsqf(v * 0x1p100f) : __builtin_amdgcn_rsqf(v);
+}
+
+// g or 1, times 1 / (1 + e^-g).  -g log2(e) in two parts, the second into the
+// exponential as its derivative: within a few units however large g is.
+__device__ __forceinline__ float gate_of(float g, int silu) {
+  const float near = g > 104.f ? 104.f : g < -104.f ? -104.f : g;  // (beyond, the exponential is 0 or infinite; NaN stays)
+  const float t = near * -1.44269504f;
+  const float rest = fmaf(near, -1.44269504f, -t) + near * -1.92596299e-8f;
+  float e = __builtin_amdgcn_exp2f(t);
+  e = fmaf(e, rest * 0.693147181f, e);
+  e = t > 127.f ? __builtin_huge_valf() : e;  // (where the correction may be of something infinite)
+  return (silu ? g : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+}
+
+// A row's scale in 8 bits, and what values are multiplied by (see row_scale).
+__device__ __forceinline__ float scale_of(uint32_t most, float* inverse) {
+  const float m = __uint_as_float(most);
+  *inverse = m < 0x1p-100f ? 1.f : 448.f * __builtin_amdgcn_rcpf(m);
+  return m < 0x1p-100f ? 1.f : m * (1.f / 448.f);
+}
+
+// v of the lane that CONTROL names.
+template <int CONTROL, typename T>
+__device__ __forceinline__ T other_lane(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 15, 15, true));
+}
+// Over the TEAM threads of a row; all of them get the result.  Within a wave by
+// exchanges of neighbours, quads, halves of 16 lanes, 16 lanes and halves.
+template <int TEAM, typename T, typename F>
+__device__ __forceinline__ T team_join(T v, F join, T* lds) {
+  v = join(v, other_lane<0xb1>(v));
+  v = join(v, other_lane<0x4e>(v));
+  v = join(v, other_lane<0x141>(v));
+  v = join(v, other_lane<0x140>(v));
+  if constexpr (TEAM > 16) {
+    const unsigned x = __builtin_bit_cast(unsigned, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const unsigned a0 = a[0], a1 = a[1];  // (a bit cast of a vector's element takes the first one)
+    v = join(__builtin_bit_cast(T, a0), __builtin_bit_cast(T, a1));
+    const unsigned y = __builtin_bit_cast(unsigned, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    const unsigned b0 = b[0], b1 = b[1];
+    v = join(__builtin_bit_cast(T, b0), __builtin_bit_cast(T, b1));
+  }
+  if constexpr (TEAM > 64) {
+    const int wave = static_cast<int>(threadIdx.x) >> 6;
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < TEAM / 64; ++w) v = join(v, lds[w]);
+  }
+  return v;
+}
 
 // n of the V floats at p (the rest are zero).
 template <int V>
@@ -34,44 +93,61 @@ __device__ __forceinline__ void load_gain(const float* p, int n, float (&g)[V]) 
 // power of two of neighbouring lanes; parts of whole pieces, through LDS.
 enum { PARTS_ROW = 0, PARTS_LANES = 1, PARTS_LDS = 2 };
 
-// One row per team, NP pieces per thread at most.
+// What a thread reads of a row, as it lies in memory.
+template <typename T, int V, int NP>
+struct RowPieces {
+  T x[NP][V], gate[NP][V], res[NP][V];
+};
+template <typename T, int V, int NP>
+__device__ __forceinline__ void load_pieces(const T* p, int cols, int first, int step, T (&t)[NP][V]) {
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const int c = first + k * step, n = cols - c;
+    if (n >= V) {
+      __builtin_memcpy(t[k], p + c, sizeof(t[k]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) t[k][i] = i < n ? p[c + i] : static_cast<T>(0);
+    }
+  }
+}
+
+// One row per team, NP pieces per thread at most: one, but for the longest rows,
+// as many waves with all of their reads on the way at once are what hides the
+// memory's latency.
 template <int DT, int OUT, int TEAM, int NP, int PARTS>
-__global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(const BlockArgs a) {
+__global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(const BlockArgs a) {
   using T = typename Elt<DT>::T;
+  using Y = typename OutElt<OUT>::T;
   constexpr int V = Piece<DT>::V;
-  constexpr int TEAMS = TEAM >= 256 ? 1 : 256 / TEAM;
-  static_assert(TEAM <= 64 || TEAM >= 256, "a team is part of a wave, or the block");
-  static_assert(PARTS != PARTS_LDS || TEAM >= 256, "sums of parts in LDS are the block's");
-  __shared__ float lds_a[TEAM > 64 ? TEAM / 64 : 1], lds_b[TEAM > 64 ? TEAM / 64 : 1];
-  __shared__ uint32_t lds_max[TEAM > 64 ? TEAM / 64 : 1];
+  constexpr int TEAMS = TEAM > 64 ? 1 : 256 / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1;
+  static_assert(PARTS != PARTS_LDS || TEAM > 64, "sums of parts in LDS are the block's");
+  __shared__ float lds_a[WAVES], lds_b[WAVES];
+  __shared__ uint32_t lds_max[WAVES];
   __shared__ float lds_part[PARTS == PARTS_LDS ? TEAM * NP : 1], lds_inv[PARTS == PARTS_LDS ? TEAM * NP : 1];
   const int t = static_cast<int>(threadIdx.x) % TEAM;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * TEAMS + static_cast<int>(threadIdx.x) / TEAM;
   if (row >= a.rows) return;  // whole teams; a team of several waves is the block
-  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-
-  float h[NP][V], g[NP][V], r[NP][V];
+  // (Values past the row's last are zero all the way, or NaN where all of the row is.)
+  RowPieces<T, V, NP> now;
+  load_pieces(static_cast<const T*>(a.x) + row * a.x_stride, a.cols, t * V, TEAM * V, now.x);
+  if (a.gate) load_pieces(static_cast<const T*>(a.gate) + row * a.gate_stride, a.cols, t * V, TEAM * V, now.gate);
+  if (a.res) load_pieces(static_cast<const T*>(a.res) + row * a.res_stride, a.cols, t * V, TEAM * V, now.res);
+  float after_gain[NP][V], scale[NP][V], before_gain[NP][V];
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) after_gain[k][i] = scale[k][i] = before_gain[k][i] = 1.f;
     const int c = (k * TEAM + t) * V;
-    load_piece<DT>(x + c, a.cols - c, h[k]);
+    if (a.after_gain) load_gain<V>(a.after_gain + c, a.cols - c, after_gain[k]);
+    if (a.scale) load_gain<V>(a.scale + c, a.cols - c, scale[k]);
+    if (a.before_gain) load_gain<V>(a.before_gain + c, a.cols - c, before_gain[k]);
   }
-  if (a.gate) {
-    const T* gate = static_cast<const T*>(a.gate) + row * a.gate_stride;
+  float h[NP][V];
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
-      const int c = (k * TEAM + t) * V;
-      load_piece<DT>(gate + c, a.cols - c, g[k]);
-    }
-  }
-  if (a.res) {
-    const T* res = static_cast<const T*>(a.res) + row * a.res_stride;
+  for (int k = 0; k < NP; ++k)
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
-      const int c = (k * TEAM + t) * V;
-      load_piece<DT>(res + c, a.cols - c, r[k]);
-    }
-  }
+    for (int i = 0; i < V; ++i) h[k][i] = to_f(now.x[k][i]);
   if (a.after) {
     float inv[NP];
     if constexpr (PARTS == PARTS_ROW) {
@@ -80,8 +156,8 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
       for (int k = 0; k < NP; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) sq = fmaf(h[k][i], h[k][i], sq);
-      sq = team_reduce<TEAM>(sq, Add{}, lds_a);
-      const float one = 1.f / sqrtf(sq / static_cast<float>(a.cols) + a.eps);
+      sq = team_join<TEAM>(sq, Add{}, lds_a);
+      const float one = inverse_root(fmaf(sq, a.per_col, a.eps));
 #pragma unroll
       for (int k = 0; k < NP; ++k) inv[k] = one;
     } else {
@@ -98,7 +174,7 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
 #pragma unroll
           for (int k = 0; k < NP; ++k) sq[k] += __shfl_xor(sq[k], o, 64);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) inv[k] = 1.f / sqrtf(sq[k] / static_cast<float>(a.part) + a.eps);
+        for (int k = 0; k < NP; ++k) inv[k] = inverse_root(fmaf(sq[k], a.per_part, a.eps));
       } else {
         const int lane = t & 63;
 #pragma unroll
@@ -109,7 +185,7 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
           for (int i = lane; i < pieces; i += 64) s += lds_part[p * pieces + i];
 #pragma unroll
           for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-          if (lane == 0) lds_inv[p] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+          if (lane == 0) lds_inv[p] = inverse_root(fmaf(s, a.per_part, a.eps));
         }
         __syncthreads();
 #pragma unroll
@@ -119,33 +195,19 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] *= inv[k];
-    if (a.after_gain) {
-#pragma unroll
-      for (int k = 0; k < NP; ++k) {
-        const int c = (k * TEAM + t) * V;
-        float w[V];
-        load_gain<V>(a.after_gain + c, a.cols - c, w);
-#pragma unroll
-        for (int i = 0; i < V; ++i) h[k][i] *= w[i];
-      }
-    }
+      for (int i = 0; i < V; ++i) h[k][i] = h[k][i] * inv[k] * after_gain[k][i];
   }
   if (a.gate) {
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] *= gate_of(g[k][i], a.silu);
+      for (int i = 0; i < V; ++i) h[k][i] *= gate_of(to_f(now.gate[k][i]), a.silu);
   }
   if (a.scale) {
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
-      const int c = (k * TEAM + t) * V;
-      float w[V];
-      load_gain<V>(a.scale + c, a.cols - c, w);
+    for (int k = 0; k < NP; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] *= w[i];
-    }
+      for (int i = 0; i < V; ++i) h[k][i] *= scale[k][i];
   }
   if (a.res) {
     T* sum = static_cast<T*>(a.sum) + row * a.sum_stride;
@@ -153,7 +215,7 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
     for (int k = 0; k < NP; ++k) {
       const int c = (k * TEAM + t) * V;
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] += r[k][i];
+      for (int i = 0; i < V; ++i) h[k][i] += to_f(now.res[k][i]);
       store_piece<DT>(sum + c, a.cols - c, h[k]);
     }
   }
@@ -163,21 +225,14 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if ((k * TEAM + t) * V + i < a.cols) sq = fmaf(h[k][i], h[k][i], sq);
-    sq = team_reduce<TEAM>(sq, Add{}, lds_b);
-    const float inv = 1.f / sqrtf(sq / static_cast<float>(a.cols) + a.eps);
+        sq = fmaf(h[k][i], h[k][i], sq);
+    sq = team_join<TEAM>(sq, Add{}, lds_b);
+    const float inv = inverse_root(fmaf(sq, a.per_col, a.eps));
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
-      const int c = (k * TEAM + t) * V;
-      float w[V];
+    for (int k = 0; k < NP; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) w[i] = 1.f;
-      if (a.before_gain) load_gain<V>(a.before_gain + c, a.cols - c, w);
-#pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] *= inv * w[i];
-    }
+      for (int i = 0; i < V; ++i) h[k][i] *= inv * before_gain[k][i];
   }
-  using Y = typename OutElt<OUT>::T;
   Y* y = static_cast<Y*>(a.y) + row * a.y_stride;
   if constexpr (OUT == MAFAT_F8) {
     uint32_t most = 0;
@@ -185,11 +240,11 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void block_norm_kernel(con
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if ((k * TEAM + t) * V + i < a.cols) most = MaxBits{}(most, __float_as_uint(h[k][i]) & 0x7fffffffu);
-    most = team_reduce<TEAM>(most, MaxBits{}, lds_max);
+        most = MaxBits{}(most, __float_as_uint(h[k][i]) & 0x7fffffffu);
+    most = team_join<TEAM>(most, MaxBits{}, lds_max);
     float by;
-    const float scale = row_scale(most, &by);
-    if (t == 0) a.y_scale[row] = scale;
+    const float y_scale = scale_of(most, &by);
+    if (t == 0) a.y_scale[row] = y_scale;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
@@ -312,7 +367,7 @@ hipError_t launch(const BlockArgs& a, hipStream_t stream) {
   const bool lanes = whole && each <= 64 && (each & (each - 1)) == 0;
 #define MAFAT_BLOCK(team_, np_, parts_)                                                                      \
   do {                                                                                                       \
-    constexpr int teams = (team_) >= 256 ? 1 : 256 / (team_), block = (team_) > 256 ? (team_) : 256;         \
+    constexpr int teams = (team_) > 64 ? 1 : 256 / (team_), block = (team_) > 64 ? (team_) : 256;            \
     return by_rows<DT, OUT>(a, teams * (kThreads / block), [&](const BlockArgs& p) {                         \
       hipLaunchKernelGGL((block_norm_kernel<DT, OUT, team_, np_, parts_>),                                   \
                          dim3(static_cast<unsigned>((p.rows + teams - 1) / teams)), dim3(block), 0, stream, p); \
@@ -321,20 +376,21 @@ hipError_t launch(const BlockArgs& a, hipStream_t stream) {
   if (one) {
     if (pieces <= 16) MAFAT_BLOCK(16, 1, PARTS_ROW);
     if (pieces <= 64) MAFAT_BLOCK(64, 1, PARTS_ROW);
-    if (pieces <= 128) MAFAT_BLOCK(64, 2, PARTS_ROW);
+    if (pieces <= 128) MAFAT_BLOCK(128, 1, PARTS_ROW);
     if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_ROW);
-    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_ROW);
+    if (pieces <= 512) MAFAT_BLOCK(512, 1, PARTS_ROW);
     if (pieces <= 1024) MAFAT_BLOCK(1024, 1, PARTS_ROW);
     if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_ROW);
   } else if (lanes) {
     if (pieces <= 64) MAFAT_BLOCK(64, 1, PARTS_LANES);
     if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_LANES);
-    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_LANES);
+    if (pieces <= 512) MAFAT_BLOCK(512, 1, PARTS_LANES);
     if (pieces <= 1024) MAFAT_BLOCK(1024, 1, PARTS_LANES);
     if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_LANES);
   } else if (whole) {
     if (pieces <= 256) MAFAT_BLOCK(256, 1, PARTS_LDS);
-    if (pieces <= 512) MAFAT_BLOCK(256, 2, PARTS_LDS);
+    if (pieces <= 512) MAFAT_BLOCK(512, 1, PARTS_LDS);
+    if (pieces <= 1024) MAFAT_BLOCK(1024, 1, PARTS_LDS);
     if (pieces <= 2048) MAFAT_BLOCK(1024, 2, PARTS_LDS);
   }
 #undef MAFAT_BLOCK

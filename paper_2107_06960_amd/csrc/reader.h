@@ -130,7 +130,7 @@ struct BlockArgs {
   int64_t rows;
   int32_t cols, groups, part;  // part: columns of a group
   int32_t after, before, silu;
-  float eps;
+  float eps, per_col, per_part;  // 1 / cols, 1 / part
 };
 hipError_t launch_block_norm(int dtype, int out_dtype, const BlockArgs& a, hipStream_t stream);
 

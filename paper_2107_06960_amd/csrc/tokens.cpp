@@ -160,6 +160,8 @@ extern "C" int mafat_block_norm(const mafat_block* c, const void* x, const float
     a.rows = rows; a.cols = static_cast<int32_t>(cols);
     a.groups = c->after ? c->groups : 1;
     a.part = a.cols / a.groups;
+    a.per_col = 1.f / static_cast<float>(a.cols);
+    a.per_part = 1.f / static_cast<float>(a.part);
     a.after = c->after != 0; a.before = c->before != 0; a.silu = c->gate_act != 0; a.eps = c->eps;
     return launched(launch_block_norm(c->dtype, c->out_dtype, a, static_cast<hipStream_t>(stream)), "block norm");
   });
