@@ -89,6 +89,18 @@ __device__ __forceinline__ void load_gain(const float* p, int n, float (&g)[V]) 
   }
 }
 
+// As store_piece, past the caches.
+template <int OUT, int V>
+__device__ __forceinline__ void put_piece(typename OutElt<OUT>::T* p, int n, const float (&v)[V]) {
+  if (n >= V) {
+    typename OutElt<OUT>::T t[V];
+    store_piece<OUT>(t, V, v);
+    store_once(p, t);
+  } else {
+    store_piece<OUT>(p, n, v);
+  }
+}
+
 // How the sums of a row's parts are formed: the row is one part; a part is a
 // power of two of neighbouring lanes; parts of whole pieces, through LDS.
 enum { PARTS_ROW = 0, PARTS_LANES = 1, PARTS_LDS = 2 };
@@ -104,7 +116,7 @@ __device__ __forceinline__ void load_pieces(const T* p, int cols, int first, int
   for (int k = 0; k < NP; ++k) {
     const int c = first + k * step, n = cols - c;
     if (n >= V) {
-      __builtin_memcpy(t[k], p + c, sizeof(t[k]));
+      load_once(p + c, t[k]);
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) t[k][i] = i < n ? p[c + i] : static_cast<T>(0);
@@ -216,7 +228,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
       const int c = (k * TEAM + t) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) h[k][i] += to_f(now.res[k][i]);
-      store_piece<DT>(sum + c, a.cols - c, h[k]);
+      put_piece<DT>(sum + c, a.cols - c, h[k]);
     }
   }
   if (a.before) {
@@ -253,7 +265,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
     const int c = (k * TEAM + t) * V;
-    store_piece<OUT>(y + c, a.cols - c, h[k]);
+    put_piece<OUT>(y + c, a.cols - c, h[k]);
   }
 }
 

@@ -16,11 +16,25 @@
 // states that the segments start from, the last one gives the outputs.
 #include "decay_device.h"
 #include "decay_launch.h"
+#include "norm_device.h"
 
 namespace mafat {
 namespace {
 
 // ------------------------------------------------------------ single tokens
+
+// As load4 and put4 of float32, past the caches.
+__device__ __forceinline__ f32x4 load4_once(const float* p, int n) {
+  if (n < 4) return load4<float>(p, n);
+  float t[4];
+  load_once(p, t);
+  return f32x4{t[0], t[1], t[2], t[3]};
+}
+__device__ __forceinline__ void put4_once(float* p, int n, f32x4 v) {
+  if (n < 4) return put4<float>(p, n, v);
+  const float t[4] = {v[0], v[1], v[2], v[3]};
+  store_once(p, t);
+}
 
 // 64 columns of a state a block; a thread holds 4 of them in RPT of its rows.
 template <int DT, int RPT>
@@ -45,7 +59,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       const int r = r0 + 16 * i;
-      s[i] = load4<float>(state + static_cast<int64_t>(r) * a.value_dim, r < a.key_dim ? nc : 0);
+      s[i] = load4_once(state + static_cast<int64_t>(r) * a.value_dim, r < a.key_dim ? nc : 0);
     }
   } else {
     const float f = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
@@ -94,7 +108,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       const int r = r0 + 16 * i;
-      if (r < a.key_dim) put4<float>(state + static_cast<int64_t>(r) * a.value_dim, nc, s[i]);
+      if (r < a.key_dim) put4_once(state + static_cast<int64_t>(r) * a.value_dim, nc, s[i]);
     }
   }
 }
@@ -403,14 +417,15 @@ DecayPlan plan_decay(const mafat_decay& c) {
   DecayPlan p{};
   // One or two tokens a request, if they are alike: a chunk would be nearly empty.
   p.recurrent = c.rows <= 2 * int64_t{c.requests};
-  // Segments of 256 tokens at least that leave two blocks a CU, all of them at once: one
+  // Segments that leave two blocks a CU, all of them at once: one
   // more would make the call take twice as long.  A request adds a segment that is not
   // full.  With that many requests alone, twice their mean length.
   const int columns = c.dtype == MAFAT_BF16 && c.key_dim % 8 == 0 && c.value_dim % 8 == 0 ? 128 : 64;  // of a block, mostly
   const int64_t slices = (c.value_dim + columns - 1) / columns;
   const int64_t most = 512 / (c.kv_heads * slices);
   int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
-  len = len < 256 ? 256 : (len + 31) / 32 * 32;
+  const int64_t least = columns == 128 ? 256 : 64;  // a chunk takes 1 us in decay_bf16.hip, 3 to 7 here
+  len = len < least ? least : (len + 31) / 32 * 32;
   p.segment = len;
   p.segments = c.rows / len + c.requests;
   p.split = !p.recurrent && c.rows > len;

@@ -56,25 +56,28 @@ __device__ __forceinline__ u32x4 scalar_range(const void* p, unsigned bytes) {
   for (int i = 0; i < 4; ++i) r[i] = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(v[i])));
   return r;
 }
+__device__ __forceinline__ unsigned scalar(unsigned v) {  // the same in all lanes, which the compiler has to know
+  return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
+}
 __device__ __forceinline__ void load16_at(const u32x4& r, unsigned off, unsigned at, unsigned to) {
   unsigned m0;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
                : "=&s"(m0)
-               : "s"(to), "v"(off), "s"(r), "s"(at)
+               : "s"(scalar(to)), "v"(off), "s"(r), "s"(scalar(at))
                : "memory");
 }
 __device__ __forceinline__ void load16_at2(const u32x4& r, unsigned off0, unsigned off1, unsigned at, unsigned to0, unsigned to1) {
   unsigned m0;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %3, %5, %6 offen lds\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds\n\ts_mov_b32 m0, %0"
                : "=&s"(m0)
-               : "s"(to0), "s"(to1), "v"(off0), "v"(off1), "s"(r), "s"(at)
+               : "s"(scalar(to0)), "s"(scalar(to1)), "v"(off0), "v"(off1), "s"(r), "s"(scalar(at))
                : "memory");
 }
 __device__ __forceinline__ void load4_at(const u32x4& r, unsigned off, unsigned at, unsigned to) {
   unsigned m0;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dword %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
                : "=&s"(m0)
-               : "s"(to), "v"(off), "s"(r), "s"(at)
+               : "s"(scalar(to)), "v"(off), "s"(r), "s"(scalar(at))
                : "memory");
 }
 
@@ -163,15 +166,18 @@ __device__ __forceinline__ double scan32(double v, double* all) {
 }
 
 // Chunks are asked for SLOTS - 1 iterations ahead, an iteration being a chunk and
-// a query head of the group: the memory's answer takes longer than one.
+// a query head of the group.  An iteration's outputs go through LDS, so that they
+// leave in the next one in whole rows of the block's columns and past the caches
+// (16384 ragged rows of 16 heads of 128: 74 us; 64 bytes of a row at a time 79,
+// and past the caches 101).
 template <int KP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
   constexpr bool OUT = MODE == DECAY_OUTPUTS;
-  constexpr int SLOTS = OUT ? 3 : 4;
+  constexpr int SLOTS = OUT ? 2 : 4;
   constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH, DTILE = NW * 256;
   constexpr int AHEAD = 4, TAHEAD = KT < 4 ? KT : 4;  // steps and tiles whose fragments are asked for at once
-  __shared__ __align__(1024) unsigned char smem[SLOTS * (KTILE + VTILE + DTILE + (OUT ? KTILE : 0))];
+  __shared__ __align__(1024) unsigned char smem[SLOTS * (KTILE + VTILE + DTILE + (OUT ? KTILE : 0)) + (OUT ? 2 * VTILE : 0)];
   __shared__ __align__(16) float table[NW][2][C];  // of each wave: c_j, and the values' weights
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -191,6 +197,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   unsigned char* const sv = sk + SLOTS * KTILE;
   unsigned char* const sd = sv + SLOTS * VTILE;  // the tokens' decays, for each wave
   unsigned char* const sq = sd + SLOTS * DTILE;
+  unsigned char* const sy = sq + SLOTS * KTILE;  // outputs, by turns
   TileFetch<KPITCH, NW> fk, fq;
   TileFetch<VPITCH, NW> fv;
   constexpr int LOADS_Q = OUT ? TileFetch<KPITCH, NW>::LOADS : 0;
@@ -280,13 +287,20 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   wait_loads();
   double total = 0.0, lag = 0.0;  // of the segment's decays, in base 2; A
   int kv_slot = 0, q_slot = 0;
-  u32x4 done[2] = {};  // outputs of the last chunk, still to be written
+  // The last iteration's outputs: where their first row goes, and how many there are.
   uint16_t* done_at = nullptr;
+  int done_rows = 0, done_slot = 0;
   auto write_done = [&] {
-    if (done_at) {
+    constexpr int PER = VPITCH / 16, ROWS = 64 / PER;
+    const unsigned char* from = sy + (done_slot ^ 1) * VTILE;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (c0 + 32 * wave + 16 * i + 8 * h < a.value_dim) __builtin_memcpy(done_at + 16 * i, &done[i], 16);
+    for (int i = 0; i < 2; ++i) {
+      const int r = ROWS * (i * NW + wave) + lane / PER, at = 8 * ((lane % PER) ^ turn<VPITCH>(r));
+      if (r < done_rows && c0 + at < a.value_dim) {
+        typedef u32x4 __attribute__((aligned(2))) loose;  // (y need not be aligned)
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(from + ROWS * (i * NW + wave) * VPITCH + 16 * lane),
+                                    reinterpret_cast<loose*>(done_at + r * a.y_row + at));
+      }
     }
   };
   auto times = [&](double log2) {
@@ -307,9 +321,8 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
       // What this iteration reads is there; what was asked for after it may be on its way
       // (loads complete in order, and stores in between only make the wait longer).
       if constexpr (OUT) {
-        if (g + 1 < heads) wait_vmcnt<LOADS_Q>();
-        else if (t + 1 < chunks) wait_vmcnt<LOADS_Q + LOADS_KV>();
-        else wait_vmcnt<0>();
+        static_assert(SLOTS == 2, "nothing that was asked for later");
+        wait_vmcnt<0>();
       } else {
         wait_stage<LOADS_KV, SLOTS - 2>(chunks - 1 - t);
       }
@@ -492,23 +505,28 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
           for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int y = 0; y < 2; ++y) w[x][y] = pack_bf16(o[8 * i + 4 * x + 2 * y] * by, o[8 * i + 4 * x + 2 * y + 1] * by);
+          u32x4 eight;
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const auto two = __builtin_amdgcn_permlane32_swap(w[0][y], w[1][y], false, false);
-            done[i][y] = two[0];
-            done[i][2 + y] = two[1];
+            eight[y] = two[0];
+            eight[2 + y] = two[1];
           }
+          *reinterpret_cast<u32x4*>(sy + done_slot * VTILE + c * VPITCH + (((4 * wave + 2 * i + h) ^ turn<VPITCH>(c)) << 4)) = eight;
         }
-        done_at = c < n ? static_cast<uint16_t*>(a.y) + (seg.first + static_cast<int64_t>(t) * C + c) * a.y_row +
-                              (kv * a.group + g) * a.y_head + c0 + 32 * wave + 8 * h
-                        : nullptr;
+        done_at = static_cast<uint16_t*>(a.y) + (seg.first + static_cast<int64_t>(t) * C) * a.y_row + (kv * a.group + g) * a.y_head + c0;
+        done_rows = n;
+        done_slot ^= 1;
         q_slot = q_slot + 1 == SLOTS ? 0 : q_slot + 1;
       }
     }
     kv_slot = kv_slot + 1 == SLOTS ? 0 : kv_slot + 1;
   }
   times(lag);
-  if constexpr (OUT) write_done();
+  if constexpr (OUT) {
+    wg_barrier_writes();
+    write_done();
+  }
   float* const to = !OUT ? part : seg.index + 1 == seg.count ? kept : nullptr;
   if (to) {
     const auto rsrc = make_rsrc(to, state_bytes);

@@ -111,7 +111,7 @@ struct RotaryArgs {
   int64_t rows;
   int32_t axes, q_heads, heads, head_dim, pairs;  // heads: of q and k together
   int32_t turning, items;  // pieces of a head that turn, and all that are moved
-  int32_t heads_each;      // heads of a thread
+  int32_t rows_each;       // rows of a block
   float magnitude;
 };
 hipError_t launch_rotary(int dtype, bool interleaved, bool in_place, RotaryArgs a, hipStream_t stream);
