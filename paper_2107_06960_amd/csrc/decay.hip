@@ -205,15 +205,19 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
         __syncthreads();
         {  // scores: a tile of 16 x 16 per wave, none above the diagonal
           const int ti = wave >> 1, tj = wave & 1;
-          f32x4 p = {0.f, 0.f, 0.f, 0.f};
+          f32x4 p = {0.f, 0.f, 0.f, 0.f}, p2 = p;  // two sums: an instruction's result takes several times its issue
           if (tj <= ti) {
 #pragma unroll
             for (int i = 0; i < KT; ++i) {
               const f32x4 x = *reinterpret_cast<const f32x4*>(&sq[(16 * ti + l16) * KP + 16 * i + 4 * h4]);
               const f32x4 y = *reinterpret_cast<const f32x4*>(&sk[(16 * tj + l16) * KP + 16 * i + 4 * h4]);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) p = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], y[r], p, 0, 0, 0);
+              for (int r = 0; r < 4; r += 2) {
+                p = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], y[r], p, 0, 0, 0);
+                p2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r + 1], y[r + 1], p2, 0, 0, 0);
+              }
             }
+            p += p2;
           }
           const int j = 16 * tj + l16;
 #pragma unroll
@@ -223,19 +227,21 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
             sp[i * PP + j] = j <= i ? p[r] * w : 0.f;
           }
         }
-        f32x4 o[2];
+        f32x4 o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) {
-          o[ti] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < KT; ++i) {
+          f32x4 x[2];
 #pragma unroll
-          for (int i = 0; i < KT; ++i) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(&sq[(16 * ti + l16) * KP + 16 * i + 4 * h4]);
+          for (int ti = 0; ti < 2; ++ti) x[ti] = *reinterpret_cast<const f32x4*>(&sq[(16 * ti + l16) * KP + 16 * i + 4 * h4]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], s[i][r], o[ti], 0, 0, 0);
-          }
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) o[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[ti][r], s[i][r], o[ti], 0, 0, 0);
+        }
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti)
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[ti][r] *= __builtin_amdgcn_exp2f(static_cast<float>(sc[16 * ti + 4 * h4 + r]));
-        }
         __syncthreads();
         if (odd) {  // a later token's value must not reach a row, not even times zero
 #pragma unroll

@@ -10,6 +10,14 @@ attend to them:
     delta = norm(o) Wo^T (+ the request's adapter)  add_rms_norm, linear8
 
 per layer, and a last norm.  Every layer reads the same keys and values, where the network left them.
+
+A layer may first mix the tokens of each request, in order, by a memory of constant size that the request keeps:
+
+    q, k, v, g = norm(h) Wm^T                       add_rms_norm, linear8
+    q, k turned by the tokens' positions            rotary, in place
+    o = linear attention with decays                decay_attention, and the request's state after it
+    delta = (norm by head(o) * silu(g)) Wn^T        block_norm into 8 bits, linear8
+    h = h + scale * norm(delta), and its norm       block_norm, for the layer's own query projection
 """
 from __future__ import annotations
 
@@ -25,8 +33,9 @@ def to_f8_rows(w):
     return (w.float() / scale[:, None]).to(O.F8), scale
 
 
-def draw_params(width, q_heads, head_dim, layers, seed=0, adapters=0, rank=8, device="cuda"):
-    """Random weights of a Reader: a list of layers, and the last norm's gain."""
+def draw_params(width, q_heads, head_dim, layers, seed=0, adapters=0, rank=8, device="cuda", mix_heads=0, mix_dim=0):
+    """Random weights of a Reader: a list of layers, and the last norm's gain.  With mix_heads heads of mix_dim, every layer
+    mixes the requests' tokens first."""
     gen = torch.Generator().manual_seed(seed)
     inner = q_heads * head_dim
 
@@ -45,15 +54,27 @@ def draw_params(width, q_heads, head_dim, layers, seed=0, adapters=0, rank=8, de
     def gain(n):
         return (1 + 0.1 * randn(n)).to(device)
 
-    return {"layers": [{"gain": gain(width), "q": linear(inner, width), "o_gain": gain(inner), "o": linear(width, inner)}
-                       for _ in range(layers)], "gain": gain(width)}
+    def mix():
+        n = mix_heads * mix_dim
+        # heads that forget within some ten to some thousand tokens
+        decay = torch.log1p(-2.0 ** -(4 + 6 * torch.arange(mix_heads) / max(mix_heads - 1, 1)))
+        return {"gain": gain(width), "qkvg": linear(4 * n, width), "log_decay": decay.to(device), "o_gain": gain(n),
+                "o": linear(width, n), "after_gain": gain(width), "scale": (0.5 + 0.1 * randn(width)).to(device)}
+
+    params = {"layers": [{"gain": gain(width), "q": linear(inner, width), "o_gain": gain(inner), "o": linear(width, inner)}
+                         for _ in range(layers)], "gain": gain(width)}
+    if mix_heads:
+        for p in params["layers"]:
+            p["mix"] = mix()
+    return params
 
 
 class Reader:
     """Layers of cross attention from rows of tokens to the feature maps of a batch of frames."""
 
-    def __init__(self, params, q_heads, kv_heads, head_dim, eps=1e-6):
+    def __init__(self, params, q_heads, kv_heads, head_dim, eps=1e-6, mix_heads=0, mix_dim=0):
         self.params, self.q_heads, self.kv_heads, self.head_dim, self.eps = params, q_heads, kv_heads, head_dim, eps
+        self.mix_heads, self.mix_dim, self._turns = mix_heads, mix_dim, {}
 
     def states(self, y):
         """Keys and values, [frames, positions, kv_heads, head_dim] each, in a network's output [frames, h, w, channels]."""
@@ -63,12 +84,43 @@ class Reader:
         kv = y.view(frames, h * w, 2, self.kv_heads, self.head_dim)
         return kv[:, :, 0], kv[:, :, 1]
 
-    def run(self, tokens, y, q_offsets=None, row_adapter=None, k_lengths=None, key_mask=None):
+    def memory(self, slots, device="cuda"):
+        """Empty memories of `slots` requests for layers that mix: float32 [layers, slots, mix_heads, mix_dim, mix_dim]."""
+        return torch.zeros(len(self.params["layers"]), slots, self.mix_heads, self.mix_dim, self.mix_dim, device=device)
+
+    def _turns_on(self, device):
+        if device not in self._turns:  # once for a device
+            self._turns[device] = O.rotary_turns(self.mix_dim // 2, device=device)
+        return self._turns[device]
+
+    def _mix(self, p, h, x, scale, next_gain, positions, offsets, states, slots):
+        """The sum after the tokens of each request are mixed, and its norm in 8 bits with `next_gain`."""
+        rows, heads, dim = h.shape[0], self.mix_heads, self.mix_dim
+        n = heads * dim
+        all_ = O.linear8(x, scale, p["qkvg"]["w"], p["qkvg"]["scale"])
+        q, k, v = (all_[:, i * n:(i + 1) * n].view(rows, heads, dim) for i in range(3))
+        O.rotary(q, positions, self._turns_on(h.device), k=k, in_place=True)
+        o = O.decay_attention(q, k, v, p["log_decay"], states=states, slots=slots, offsets=offsets)
+        _, x, scale = O.block_norm(o.view(rows, n), after_gain=p["o_gain"], groups=heads, gate=all_[:, 3 * n:], before=False,
+                                   eps=self.eps)
+        delta = O.linear8(x, scale, p["o"]["w"], p["o"]["scale"])
+        return O.block_norm(delta, after_gain=p["after_gain"], scale=p["scale"], residual=h, before_gain=next_gain, eps=self.eps)
+
+    def run(self, tokens, y, q_offsets=None, row_adapter=None, k_lengths=None, key_mask=None, positions=None, offsets=None,
+            memory=None, slots=None):
         """tokens: bfloat16 [rows, width], as y has to be, frame by frame; q_offsets: int32 [frames + 1], the frames' rows (None: as many
         each); row_adapter: int32 [rows], the adapter of each row's request, for layers that have adapters (None: without
-        them).  Returns the normed rows."""
+        them).  For layers that mix: positions: int32 [rows], of the tokens in their requests; offsets: int32 [requests + 1],
+        the requests' rows (None: as many each); memory: what memory() gives, updated in place (None: every request starts
+        without one, and none is kept); slots: int32 [requests], each request's place in it (None: request i has place i).
+        Returns the normed rows."""
         if row_adapter is not None and not any(p[i]["adapters"] for p in self.params["layers"] for i in ("q", "o")):
             raise ValueError("row_adapter names adapters, but no layer has any")
+        mixes = any("mix" in p for p in self.params["layers"])
+        if mixes and (positions is None or not self.mix_heads):
+            raise ValueError("layers that mix need positions, and a reader with mix_heads and mix_dim")
+        if not mixes and any(t is not None for t in (positions, offsets, memory, slots)):
+            raise ValueError("positions, offsets, memory and slots are for layers that mix, but no layer does")
         k, v = self.states(y)
         rows, h, delta = tokens.shape[0], tokens, None
 
@@ -76,11 +128,15 @@ class Reader:
             ad = p["adapters"] if row_adapter is not None else None
             return O.linear8(x, scale, p["w"], p["scale"], adapters=ad, row_adapter=row_adapter if ad is not None else None)
 
-        for p in self.params["layers"]:
+        for i, p in enumerate(self.params["layers"]):
+            gain = p["mix"]["gain"] if "mix" in p else p["gain"]
             if delta is None:
-                _, x, scale = O.add_rms_norm(h, p["gain"], eps=self.eps)
+                _, x, scale = O.add_rms_norm(h, gain, eps=self.eps)
             else:
-                h, x, scale = O.add_rms_norm(delta, p["gain"], h, eps=self.eps)
+                h, x, scale = O.add_rms_norm(delta, gain, h, eps=self.eps)
+            if "mix" in p:
+                h, x, scale = self._mix(p["mix"], h, x, scale, p["gain"], positions, offsets,
+                                        None if memory is None else memory[i], slots)
             q = linear(x, scale, p["q"]).view(rows, self.q_heads, self.head_dim)
             o, _ = O.cross_attention(q, k, v, q_offsets=q_offsets, k_lengths=k_lengths, key_mask=key_mask)
             _, x, scale = O.add_rms_norm(o.view(rows, -1), p["o_gain"], eps=self.eps)
