@@ -263,8 +263,11 @@ typedef struct {
  * States and sums are float32.  Long requests are cut into segments whose states
  * are joined, so the last bits of a row may depend on the sizes of the call.  What is
  * not finite in a token reaches its own request's rows from that token on, and its
- * state.  In bfloat16, scores and the states that rows read enter the matrix
- * products in bfloat16 parts; the states that are kept do not lose by it.  Errors:
+ * state.  In bfloat16, where heads, addresses and strides are whole 16 bytes and
+ * requests have more than two rows, scores and the states that rows read are
+ * rounded to bfloat16 (2.3e-3 of the output's norm against float64, of which 1.7e-3
+ * is the output's own rounding); the states that are kept are not.  There what a
+ * token adds to the state overflows above 2e31, 2^-24 of float32's largest.  Errors:
  * EINVAL (null or misaligned pointer, bad size or stride, rows not divisible
  * without offsets, scale not finite, an output overlapping another tensor),
  * EWORKSPACE, EUNSUPPORTED (dtype, key_dim or value_dim > 256, rows * q_heads or

@@ -47,10 +47,11 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
   const int slice = id - rh * a.slices;
   const int request = static_cast<int>(static_cast<uint32_t>(rh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = rh - request * a.kv_heads;
+  const int ahead = slots_ahead(a);
   int first, n;
   rows_of(a, request, &first, &n);
   if (n == 0) return;
-  const int64_t slot = slot_of(a, request);
+  const int64_t slot = slot_of(a, request, ahead);
   const int c = 64 * slice + 4 * (tid & 15), nc = a.value_dim - c, r0 = tid >> 4;
   float* state = nullptr;
   f32x4 s[RPT];
@@ -141,10 +142,11 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   const int bh = id - slice * all_bh;
   const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = bh - b * a.kv_heads;
+  const int ahead = slots_ahead(a);
   const Segment seg = find_segment(a, b);
   if (!seg.any || (MODE == DECAY_ADDS && seg.index + 1 == seg.count)) return;
   const int c0 = 64 * slice, col = c0 + 16 * wave + l16;  // of the state
-  const int64_t slot = MODE == DECAY_OUTPUTS && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
+  const int64_t slot = MODE == DECAY_OUTPUTS && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request, ahead) : SLOT_NONE;
   float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
 
@@ -317,6 +319,7 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   const int request = static_cast<int>(static_cast<uint32_t>(rh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = rh - request * a.kv_heads;
   // the request's first segment, and how many there are
+  const int ahead = slots_ahead(a);
   int first, n, length;
   rows_of(a, request, &first, &n);
   const int count = segments_of(a, n, &length);
@@ -333,8 +336,9 @@ __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) b += static_cast<uint32_t>(__shfl_xor(static_cast<int>(b), o, 64));
   }
-  if (b + static_cast<uint32_t>(count) > static_cast<uint32_t>(a.segments)) return;  // (offsets that decrease)
-  const int64_t slot = slot_of(a, request);
+  const uint32_t room = static_cast<uint32_t>(a.segments);
+  if (b > room || static_cast<uint32_t>(count) > room - b) return;  // (offsets that decrease)
+  const int64_t slot = slot_of(a, request, ahead);
   if (e >= size) return;
   const float start = slot == SLOT_TAKEN ? __builtin_nanf("") : 0.f;
   fv s;
@@ -431,7 +435,7 @@ DecayPlan plan_decay(const mafat_decay& c) {
   const int64_t most = 512 / (c.kv_heads * slices);
   int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
   const int64_t least = columns == 128 ? 256 : 64;  // a chunk takes 1 us in decay_bf16.hip, 3 to 7 here
-  len = len < least ? least : (len + 31) / 32 * 32;
+  len = len < least ? least : len > 8192 ? 8192 : (len + 31) / 32 * 32;  // (extents of a segment are 31 bits wide)
   p.segment = len;
   p.segments = c.rows / len + c.requests;
   p.split = !p.recurrent && c.rows > len;

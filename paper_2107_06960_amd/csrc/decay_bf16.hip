@@ -188,6 +188,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   const int bh = id - slice * all_bh;
   const int b = static_cast<int>(static_cast<uint32_t>(bh) / static_cast<uint32_t>(a.kv_heads));
   const int kv = bh - b * a.kv_heads;
+  const int ahead = slots_ahead(a);
   const Segment seg = find_segment(a, b);
   if (!seg.any || (!OUT && seg.index + 1 == seg.count)) return;
 
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   for (int i = 0; i < SLOTS - 1; ++i)
     if (ask_t < chunks) ask();
 
-  const int64_t slot = OUT && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request) : SLOT_NONE;
+  const int64_t slot = OUT && (seg.index == 0 || seg.index + 1 == seg.count) ? slot_of(a, seg.request, ahead) : SLOT_NONE;
   float* const kept = slot >= 0 ? a.states + slot * a.state_slot + static_cast<int64_t>(kv) * a.key_dim * a.value_dim : nullptr;
   float* const part = a.part + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.key_dim * a.value_dim;
   // The state's entries by a descriptor: what is past its rows or columns reads as

@@ -30,19 +30,26 @@ __device__ __forceinline__ void rows_of(const DecayArgs& a, int i, int* first, i
   *n = max(min(max(a.offsets[i + 1], 0), a.rows) - *first, 0);
 }
 
+// Slot of request `lane`: asked for ahead of slot_of, beside what else a kernel
+// starts with, since loads that wait for each other are what its start takes.
+__device__ __forceinline__ int slots_ahead(const DecayArgs& a) {
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  return a.states && a.slots && lane < a.requests ? a.slots[lane] : -1;
+}
 // The state of a request's slot: NONE: starts from zeros and is not kept;
 // TAKEN: an earlier request with rows has it.  The same in all lanes.
 enum { SLOT_NONE = -1, SLOT_TAKEN = -2 };
-__device__ __forceinline__ int64_t slot_of(const DecayArgs& a, int request) {
+__device__ __forceinline__ int64_t slot_of(const DecayArgs& a, int request, int ahead) {
   if (!a.states) return SLOT_NONE;
-  const int s = a.slots ? a.slots[request] : request;
+  int s = request;
+  if (a.slots) s = request < 64 ? __builtin_amdgcn_readlane(ahead, request) : a.slots[request];
   if (s < 0 || s >= a.pool) return SLOT_NONE;
   if (a.slots) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     for (int e0 = 0; e0 < request; e0 += 64) {
       const int e = e0 + lane;
       bool same = false;
-      if (e < request && a.slots[e] == s) {
+      if (e < request && (e0 == 0 ? ahead : a.slots[e]) == s) {
         int first, n;
         rows_of(a, e, &first, &n);
         same = n > 0;

@@ -225,7 +225,8 @@ extern "C" int mafat_decay_attention(const mafat_decay* c, const void* q, const 
     a.decay_by_row = c->decay_by_row != 0;
     a.segment = static_cast<int32_t>(p.split ? p.segment : c->rows);
     a.segments = static_cast<int32_t>(p.split ? p.segments : c->requests);
-    if (!offsets) a.segments = c->requests * ((a.per_request + a.segment - 1) / a.segment);  // known, and no more than that
+    if (!offsets)  // known, and no more than that
+      a.segments = static_cast<int32_t>(c->requests * ((int64_t{a.per_request} + a.segment - 1) / a.segment));
     if (p.split) a.factor = a.part + p.segments * size;
     a.scale = c->scale;
     return launched(launch_decay(c->dtype, a, p, static_cast<hipStream_t>(stream)), "decay attention");

@@ -485,7 +485,9 @@ def block_norm(x, after=True, after_gain=None, groups=1, gate=None, act="silu", 
     if to is F8:
         y_scale = torch.empty(rows, dtype=torch.float32, device=dev)
         y_scale_at = y_scale.data_ptr()
-    ref, _ = _block_shape(dt, to, rows, cols, bool(after), groups, act == "silu", bool(before), eps, x_stride, g_stride, r_stride)
+    # (of a tensor its value now: the shapes below are kept by what they hold)
+    ref, _ = _block_shape(dt, to, rows, cols, bool(after), int(groups), act == "silu", bool(before), float(eps), x_stride, g_stride,
+                          r_stride)
     _call("mafat_block_norm", dev.index, ref, x.data_ptr(), after_at, gate_at, scale_at, res_at, h_at, before_at, y.data_ptr(),
           y_scale_at)
     return h, y, y_scale

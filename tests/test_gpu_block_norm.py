@@ -159,6 +159,20 @@ def test_gates_far_out():
 
 
 @pytest.mark.gpu
+def test_eps_in_a_tensor_is_read_at_every_call():
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    x, _, res, a, s, b = _tensors(3, 64, "f32", 5)
+    eps = torch.tensor(1e-6)
+    for value in (1e-6, 0.5, 1e-6):
+        eps.fill_(value)
+        got = O.block_norm(x, eps=eps, out="f32")[1]
+        assert torch.equal(got, O.block_norm(x, eps=eps.item(), out="f32")[1])
+    assert not torch.equal(got, O.block_norm(x, eps=0.5, out="f32")[1])
+
+
+@pytest.mark.gpu
 def test_python_refusals():
     require_gpu()
     from paper_2107_06960_amd import mafat as M

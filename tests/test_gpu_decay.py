@@ -274,6 +274,41 @@ def test_what_is_not_finite_reaches_later_rows_of_its_request_only(n, at, where,
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rate", [2.0, 30.0])
+def test_what_is_not_finite_where_heads_forget_fast(rate, dtype):
+    """Chunks that forget more than their sums are kept for, with values that are not finite in the middle."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    x = _inputs(500, 4, 2, 64, 64, dtype, 9, pool=1, rate=rate)
+    clean, _ = _check(x)
+    x["v"][333, 1, 7] = math.nan
+    x["v"][340, 1, 9] = math.inf
+    y = O.decay_attention(x["q"], x["k"], x["v"], x["log_decay"], states=x["states"].clone())
+    other = torch.ones_like(y, dtype=torch.bool)
+    other[333:, 2:, 7] = False
+    other[340:, 2:, 9] = False
+    tight = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -18
+    assert torch.isfinite(y[other]).all() and torch.isnan(y[333, 2:, 7]).all() and not torch.isfinite(y[340, 2:, 9]).any()
+    assert _norm((y[other] - clean[other]).double()) <= tight * _norm(clean[other].double())
+
+
+@pytest.mark.gpu
+def test_offsets_that_decrease_stay_inside():
+    """Which rows are computed is open then, but nothing outside of the tensors is touched, and what follows is right."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    x = _inputs(700, 2, 1, 64, 64, "bf16", 3, pool=4)
+    for off in ([0, 700, 0, 700, 0], [700, 0, 350, 100, 700], [-5, 2000, -7, 300, 1 << 30]):
+        O.decay_attention(x["q"], x["k"], x["v"], x["log_decay"], states=x["states"].clone(),
+                          offsets=torch.tensor(off, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    _check(x, off=[0, 300, 300, 650, 700])
+
+
+@pytest.mark.gpu
 def test_chunks_and_single_tokens_agree():
     """A prompt at once, in two calls, and its last tokens one by one."""
     require_gpu()
