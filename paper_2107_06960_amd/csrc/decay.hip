@@ -425,16 +425,21 @@ hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
 
 DecayPlan plan_decay(const mafat_decay& c) {
   DecayPlan p{};
-  // One or two tokens a request, if they are alike: a chunk would be nearly empty.
-  p.recurrent = c.rows <= 2 * int64_t{c.requests};
+  // One token a request, if they are alike (two where the chunked kernel is the slow one):
+  // a chunk would be nearly empty.  (64 requests, 16 heads of 128: one token each 28.7 us;
+  // two in turn 31, four in a chunk 26.)
   // Segments that leave two blocks a CU, all of them at once: one
   // more would make the call take twice as long.  A request adds a segment that is not
   // full.  With that many requests alone, twice their mean length.
   const int columns = c.dtype == MAFAT_BF16 && c.key_dim % 8 == 0 && c.value_dim % 8 == 0 ? 128 : 64;  // of a block, mostly
+  p.recurrent = c.rows <= (columns == 128 ? 1 : 2) * int64_t{c.requests};
   const int64_t slices = (c.value_dim + columns - 1) / columns;
   const int64_t most = 512 / (c.kv_heads * slices);
   int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
-  const int64_t least = columns == 128 ? 256 : 64;  // a chunk takes 1 us in decay_bf16.hip, 3 to 7 here
+  // A chunk takes 1 us in decay_bf16.hip, 3 to 7 here, and the two launches more 8: one request of
+  // 1024 rows of 8 heads of 64 takes 30, 22 or 18 us in segments of 256, 128 or 64, of 4096 rows
+  // 32, 26 or 29; one of 130 rows 11.5 whole and 18 in two.
+  const int64_t least = columns == 64 ? 64 : c.rows <= 256 ? 256 : 128;
   len = len < least ? least : len > 8192 ? 8192 : (len + 31) / 32 * 32;  // (extents of a segment are 31 bits wide)
   p.segment = len;
   p.segments = c.rows / len + c.requests;
