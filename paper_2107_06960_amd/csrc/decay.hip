@@ -165,6 +165,38 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 #pragma unroll
     for (int i = 0; i < KT; ++i) s[i] = f32x4{f, f, f, f};
   }
+  // The next chunk (and the next head's queries) are on their way in registers while
+  // one is worked on.
+  constexpr int KN = C * 4 * KT / 256, VN = C * 16 / 256;
+  f32x4 next_k[KN], next_v[VN], next_q[MODE == DECAY_OUTPUTS ? KN : 1];
+  float next_decay = 0.f;
+  const auto ask = [&](int t0) {
+    const int n = min(C, seg.n - t0);
+    const int64_t row0 = seg.first + t0;
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int e = tid + 256 * i, r = e / (4 * KT), d = 4 * (e % (4 * KT));
+      next_k[i] = load4<T>(static_cast<const T*>(a.k) + (row0 + r) * a.k_row + kv * a.k_head + d, r < n ? a.key_dim - d : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      const int e = tid + 256 * i, r = e >> 4, d = 4 * (e & 15);
+      next_v[i] = load4<T>(static_cast<const T*>(a.v) + (row0 + r) * a.v_row + kv * a.v_head + c0 + d, r < n ? a.value_dim - c0 - d : 0);
+    }
+    next_decay = lane < n ? a.log_decay[(a.decay_by_row ? (row0 + lane) * a.decay_row : 0) + kv] : 0.f;
+  };
+  const auto ask_q = [&](int t0, int h) {
+    const int n = min(C, seg.n - t0);
+    const int64_t row0 = seg.first + t0;
+#pragma unroll
+    for (int i = 0; i < (MODE == DECAY_OUTPUTS ? KN : 0); ++i) {
+      const int e = tid + 256 * i, r = e / (4 * KT), d = 4 * (e % (4 * KT));
+      next_q[i] = load4<T>(static_cast<const T*>(a.q) + (row0 + r) * a.q_row + (kv * a.group + h) * a.q_head + d,
+                           r < n ? a.key_dim - d : 0);
+    }
+  };
+  ask(0);
+  ask_q(0, 0);
   double total = 0.0;
   for (int t0 = 0; t0 < seg.n; t0 += C) {
     const int n = min(C, seg.n - t0);
@@ -172,22 +204,24 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
     __syncthreads();
     if (tid == 0) odd = 0;
     __syncthreads();
-    for (int e = tid; e < C * 4 * KT; e += 256) {
-      const int r = e / (4 * KT), d = 4 * (e % (4 * KT));
-      const T* p = static_cast<const T*>(a.k) + (row0 + r) * a.k_row + kv * a.k_head + d;
-      *reinterpret_cast<f32x4*>(&sk[r * KP + d]) = load4<T>(p, r < n ? a.key_dim - d : 0);
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int e = tid + 256 * i;
+      *reinterpret_cast<f32x4*>(&sk[e / (4 * KT) * KP + 4 * (e % (4 * KT))]) = next_k[i];
     }
-    for (int e = tid; e < C * 16; e += 256) {
-      const int r = e >> 4, d = 4 * (e & 15);
-      const T* p = static_cast<const T*>(a.v) + (row0 + r) * a.v_row + kv * a.v_head + c0 + d;
-      const f32x4 v = load4<T>(p, r < n ? a.value_dim - c0 - d : 0);
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      const int e = tid + 256 * i;
+      const f32x4 v = next_v[i];
       const float z = (v[0] - v[0]) + (v[1] - v[1]) + (v[2] - v[2]) + (v[3] - v[3]);
       if (!(z == 0.f)) odd = 1;
-      *reinterpret_cast<f32x4*>(&sv[r * VP + d]) = v;
+      *reinterpret_cast<f32x4*>(&sv[(e >> 4) * VP + 4 * (e & 15)]) = v;
     }
+    const float decay = next_decay;
+    if (t0 + C < seg.n) ask(t0 + C);
     if (wave == 0) {
       double g = 0.0;
-      if (lane < n) g = decay_log2(a.log_decay[(a.decay_by_row ? (row0 + lane) * a.decay_row : 0) + kv]);
+      if (lane < n) g = decay_log2(decay);
 #pragma unroll
       for (int o = 1; o < C; o <<= 1) {
         const double left = __shfl_up(g, o, 64);
@@ -199,11 +233,13 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
     if constexpr (MODE == DECAY_OUTPUTS) {
       for (int h = 0; h < a.group; ++h) {
         const int head = kv * a.group + h;
-        for (int e = tid; e < C * 4 * KT; e += 256) {
-          const int r = e / (4 * KT), d = 4 * (e % (4 * KT));
-          const T* p = static_cast<const T*>(a.q) + (row0 + r) * a.q_row + head * a.q_head + d;
-          *reinterpret_cast<f32x4*>(&sq[r * KP + d]) = load4<T>(p, r < n ? a.key_dim - d : 0);
+#pragma unroll
+        for (int i = 0; i < KN; ++i) {
+          const int e = tid + 256 * i;
+          *reinterpret_cast<f32x4*>(&sq[e / (4 * KT) * KP + 4 * (e % (4 * KT))]) = next_q[i];
         }
+        if (h + 1 < a.group) ask_q(t0, h + 1);
+        else if (t0 + C < seg.n) ask_q(t0 + C, 0);
         __syncthreads();
         {  // scores: a tile of 16 x 16 per wave, none above the diagonal
           const int ti = wave >> 1, tj = wave & 1;
@@ -434,7 +470,8 @@ DecayPlan plan_decay(const mafat_decay& c) {
   const int columns = c.dtype == MAFAT_BF16 && c.key_dim % 8 == 0 && c.value_dim % 8 == 0 ? 128 : 64;  // of a block, mostly
   p.recurrent = c.rows <= (columns == 128 ? 1 : 2) * int64_t{c.requests};
   const int64_t slices = (c.value_dim + columns - 1) / columns;
-  const int64_t most = 512 / (c.kv_heads * slices);
+  const int64_t room = c.key_dim > 128 ? 256 : 512;  // (one block a CU at larger heads)
+  const int64_t most = room / (c.kv_heads * slices);
   int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
   // A chunk takes 1 us in decay_bf16.hip, 3 to 7 here, and the two launches more 8: one request of
   // 1024 rows of 8 heads of 64 takes 30, 22 or 18 us in segments of 256, 128 or 64, of 4096 rows
