@@ -36,7 +36,9 @@ __device__ __forceinline__ void put4_once(float* p, int n, f32x4 v) {
   store_once(p, t);
 }
 
-// 64 columns of a state a block; a thread holds 4 of them in RPT of its rows.
+// 64 columns of a state a block; a thread holds 4 of them in RPT of its rows, all
+// of whose reads are on the way at once.  64 requests of 16 heads of 128: 27 us,
+// 4.9 TB/s.
 template <int DT, int RPT>
 __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
   using T = typename Elt<DT>::T;
@@ -122,7 +124,9 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
 // The 16x16x4 instruction's operands hold, in lane l, row (column) l % 16 and
 // the summed axis' entry l / 16; its result column l % 16 and rows 4 (l / 16) + r.
 // So the state's tile T is the operand of q S as it stands, if step r of the
-// instruction sums over the keys' entries 16 T + 4 (l / 16) + r.
+// instruction sums over the keys' entries 16 T + 4 (l / 16) + r.  Bound by these
+// instructions, a tenth of bfloat16's rate: 4131 rows of 16 heads of 128 in float32
+// take 123 us, of 59 in bfloat16 71 (of 56, in decay_bf16.hip, 33).
 template <int DT, int KT, int MODE>
 __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   using T = typename Elt<DT>::T;
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 
 // What segments add -> what they start from, for requests of several segments.
 // A thread takes V entries of a head's state through the segments, with the next
-// AHEAD of them on their way.
+// AHEAD of them on their way.  (121 segments of 4 heads of 128: 15 us with 32 ahead, 19 with 8.)
 template <int V, int AHEAD>
 __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   typedef float fv __attribute__((ext_vector_type(V)));
