@@ -45,15 +45,22 @@ __device__ __forceinline__ int64_t slot_of(const DecayArgs& a, int request, int 
   if (a.slots) s = request < 64 ? __builtin_amdgcn_readlane(ahead, request) : a.slots[request];
   if (s < 0 || s >= a.pool) return SLOT_NONE;
   if (a.slots) {
+    // The requests before it, the first 64 of them from `ahead`, then 512 at a time.
     const int lane = static_cast<int>(threadIdx.x) & 63;
-    for (int e0 = 0; e0 < request; e0 += 64) {
-      const int e = e0 + lane;
+    const auto has = [&](int e, int slot) {
+      if (e >= request || slot != s) return false;
+      int first, n;
+      rows_of(a, e, &first, &n);
+      return n > 0;
+    };
+    if (__builtin_amdgcn_ballot_w64(has(lane, ahead))) return SLOT_TAKEN;
+    for (int e0 = 64; e0 < request; e0 += 512) {
+      int slot[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) slot[i] = e0 + 64 * i + lane < request ? a.slots[e0 + 64 * i + lane] : -1;
       bool same = false;
-      if (e < request && (e0 == 0 ? ahead : a.slots[e]) == s) {
-        int first, n;
-        rows_of(a, e, &first, &n);
-        same = n > 0;
-      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) same |= has(e0 + 64 * i + lane, slot[i]);
       if (__builtin_amdgcn_ballot_w64(same)) return SLOT_TAKEN;
     }
   }

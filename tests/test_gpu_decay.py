@@ -6,8 +6,9 @@ c 2^-c is, 0.54); n such roundings in any order stay below n e of the sum of mag
 are independent.  So singly: (dk + n + 64) e of the sums of magnitudes, n the tokens; as a whole: the norm of the error
 below 4 sqrt(dk + n + 64) e of the norm of what the sums of magnitudes would be if signs did not cancel at all, which for
 random signs is the norm of the value itself.  bfloat16 outputs add their own rounding, 2^-8, and the kernel for whole tiles
-rounds scores and, in two parts of 2^-9 each, states and weighted values: 2^-8 of the scores' part and 2^-16 of the rest, again
-as independent errors: three roundings of 2^-8 bound the outputs as a whole; states stay within 2^-16."""
+rounds scores, and the states that rows read, to bfloat16, again 2^-8 each as independent errors: three roundings of 2^-8
+bound the outputs as a whole.  Its states stay within 2^-16: weighted values enter them in parts that leave 2^-17 of a term
+or less."""
 import math
 
 import pytest
@@ -165,6 +166,17 @@ def test_many_requests_and_the_same_slot(dtype):
         slots = [r.randrange(-1, 200) for _ in range(150)]
         x = _inputs(rows, 2, 1, 32, 32, dtype, 7, pool=199)
         _check(x, off=[0] + off + [rows], slots=slots)
+
+
+@pytest.mark.gpu
+def test_a_slot_that_a_request_far_before_has():
+    """Past the first 64 requests and the 512 after them."""
+    require_gpu()
+    x = _inputs(1400, 1, 1, 16, 16, "f32", 11, pool=1400)
+    slots = list(range(1400))
+    for later, earlier in ((63, 0), (64, 63), (65, 64), (575, 64), (576, 575), (577, 0), (1399, 576), (1398, 1100), (1000, 999)):
+        slots[later] = slots[earlier]
+    _check(x, slots=slots)
 
 
 @pytest.mark.gpu
