@@ -26,9 +26,10 @@
 // What a weighted value loses in bfloat16 goes along as further bfloat16 parts: the
 // states that are kept and joined are float32 and have to be near float32's accuracy
 // after any number of chunks (three parts of a value: 2^-27 of it; two parts left
-// states 2e-6 off).  Scores, and states where rows read them, are rounded once: they
-// end in an output that is rounded alike (a second part of the states takes 10 %
-// more time and brings outputs from 2.3e-3 to 1.8e-3 of their norm).
+// states 2e-6 off).  Scores, and states where rows of large calls read them, are
+// rounded once: they end in an output that is rounded alike.  FINE: those states in
+// two parts, which brings outputs from 2.3e-3 to 1.8e-3 of their norm and takes large
+// calls 10 to 15 % more time (16384 ragged rows of 16 heads of 128: 117 and 132 us).
 #include "cross_fast.h"
 #include "decay_device.h"
 #include "decay_launch.h"
@@ -38,6 +39,7 @@ namespace {
 
 constexpr int C = 32;         // tokens of a chunk
 constexpr double kLag = 24.0;  // of A, in base 2
+constexpr int64_t kFineRows = 65536;  // rows times key/value heads of a call, 8 chunks a CU
 
 // Byte offset of row r in a tile of PITCH-byte rows; position p of a row holds
 // the 16-byte piece p ^ turn(r).  Reads of a row per lane (16 lanes at a time)
@@ -173,7 +175,7 @@ __device__ __forceinline__ double scan32(double v, double* all) {
 // leave in the next one in whole rows of the block's columns and past the caches
 // (16384 ragged rows of 16 heads of 128: 74 us; 64 bytes of a row at a time 79,
 // and past the caches 101).
-template <int KP, int NW, int MODE>
+template <int KP, int NW, int MODE, bool FINE>
 __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
   constexpr bool OUT = MODE == DECAY_OUTPUTS;
@@ -390,11 +392,18 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         for (int i = 0; i < 16; ++i) p[i] = o[i] = 0.f;
 #pragma unroll
         for (int x = 0; x < STEPS; ++x) {
-          u32x4 sf;
+          constexpr int PARTS = FINE ? 2 : 1;
+          u32x4 sf[PARTS];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sf[i] = pack_bf16(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1]);
+          for (int i = 0; i < 4; ++i) {
+            uint32_t part2[PARTS];
+            split(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1], part2);
+#pragma unroll
+            for (int y = 0; y < PARTS; ++y) sf[y][i] = part2[y];
+          }
           Tile<MAFAT_BF16>::mul(p, kf[x % AHEAD], qf[x % AHEAD]);
-          Tile<MAFAT_BF16>::mul(o, sf, qf[x % AHEAD]);
+#pragma unroll
+          for (int y = 0; y < PARTS; ++y) Tile<MAFAT_BF16>::mul(o, sf[y], qf[x % AHEAD]);
           if (x + AHEAD < STEPS) {
             fragment(x + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
@@ -544,20 +553,20 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
     a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
 }
 
-template <int KP, int NW, int MODE>
+template <int KP, int NW, int MODE, bool FINE>
 hipError_t launch(DecayArgs a, hipStream_t stream) {
   a.slices = (a.value_dim + 32 * NW - 1) / (32 * NW);
   return for_decay_blocks(a, [&](const DecayArgs& p, unsigned n) {
-    hipLaunchKernelGGL((decay_chunk_kernel<KP, NW, MODE>), dim3(n), dim3(64 * NW), 0, stream, p);
+    hipLaunchKernelGGL((decay_chunk_kernel<KP, NW, MODE, FINE>), dim3(n), dim3(64 * NW), 0, stream, p);
   });
 }
 
-template <int MODE>
+template <int MODE, bool FINE>
 hipError_t launch_mode(const DecayArgs& a, hipStream_t stream) {
   const bool few = a.value_dim <= 64;
-  if (a.key_dim <= 64) return few ? launch<64, 2, MODE>(a, stream) : launch<64, 4, MODE>(a, stream);
-  if (a.key_dim <= 128) return few ? launch<128, 2, MODE>(a, stream) : launch<128, 4, MODE>(a, stream);
-  return few ? launch<256, 2, MODE>(a, stream) : launch<256, 4, MODE>(a, stream);
+  if (a.key_dim <= 64) return few ? launch<64, 2, MODE, FINE>(a, stream) : launch<64, 4, MODE, FINE>(a, stream);
+  if (a.key_dim <= 128) return few ? launch<128, 2, MODE, FINE>(a, stream) : launch<128, 4, MODE, FINE>(a, stream);
+  return few ? launch<256, 2, MODE, FINE>(a, stream) : launch<256, 4, MODE, FINE>(a, stream);
 }
 
 }  // namespace
@@ -573,7 +582,10 @@ bool decay_bf16_fits(const DecayArgs& a) {
 }
 
 hipError_t launch_decay_bf16(int mode, const DecayArgs& a, hipStream_t stream) {
-  return mode == DECAY_ADDS ? launch_mode<DECAY_ADDS>(a, stream) : launch_mode<DECAY_OUTPUTS>(a, stream);
+  if (mode == DECAY_ADDS) return launch_mode<DECAY_ADDS, false>(a, stream);
+  // Calls of a few chunks a CU wait for launches and memory, not for a second part of the states.
+  if (static_cast<int64_t>(a.rows) * a.kv_heads <= kFineRows) return launch_mode<DECAY_OUTPUTS, true>(a, stream);
+  return launch_mode<DECAY_OUTPUTS, false>(a, stream);
 }
 
 }  // namespace mafat

@@ -6,7 +6,7 @@ c 2^-c is, 0.54); n such roundings in any order stay below n e of the sum of mag
 are independent.  So singly: (dk + n + 64) e of the sums of magnitudes, n the tokens; as a whole: the norm of the error
 below 4 sqrt(dk + n + 64) e of the norm of what the sums of magnitudes would be if signs did not cancel at all, which for
 random signs is the norm of the value itself.  bfloat16 outputs add their own rounding, 2^-8, and the kernel for whole tiles
-rounds scores, and the states that rows read, to bfloat16, again 2^-8 each as independent errors: three roundings of 2^-8
+rounds scores, and in large calls the states that rows read, to bfloat16, again 2^-8 each as independent errors: three roundings of 2^-8
 bound the outputs as a whole.  Its states stay within 2^-16: weighted values enter them in parts that leave 2^-17 of a term
 or less."""
 import math
@@ -166,6 +166,14 @@ def test_many_requests_and_the_same_slot(dtype):
         slots = [r.randrange(-1, 200) for _ in range(150)]
         x = _inputs(rows, 2, 1, 32, 32, dtype, 7, pool=199)
         _check(x, off=[0] + off + [rows], slots=slots)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows, heads", [(4100, 16), (9000, 8)])
+def test_large_calls(rows, heads):
+    """Above 65536 rows times heads the states that rows read are rounded once."""
+    require_gpu()
+    _check(_inputs(rows, heads, heads, 32, 32, "bf16", rows, pool=2, rate=0.01), off=[0, rows // 3, rows])
 
 
 @pytest.mark.gpu
