@@ -264,10 +264,10 @@ typedef struct {
  * are joined, so the last bits of a row may depend on the sizes of the call.  What is
  * not finite in a token reaches its own request's rows from that token on, and its
  * state.  In bfloat16, where heads, addresses and strides are whole 16 bytes and
- * requests have more than one row, scores are rounded to bfloat16, and so are the
- * states that rows read where rows * kv_heads is above 65536 (below, they enter in two
- * parts): 2.3e-3 (1.8e-3) of the output's norm against float64, of which 1.7e-3
- * is the output's own rounding; the states that are kept are not.  There what a
+ * requests have more than one row, scores, and states and values where they end in
+ * an output, enter products as two bfloat16 parts each, which leave 2^-16 of a
+ * term: outputs are off by their own rounding, whatever else is in the call.  The
+ * states that are kept have float32's accuracy.  There what a
  * token adds to the state overflows above 2e31, 2^-24 of float32's largest.  Errors:
  * EINVAL (null or misaligned pointer, bad size or stride, rows not divisible
  * without offsets, scale not finite, an output overlapping another tensor),

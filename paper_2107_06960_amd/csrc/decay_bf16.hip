@@ -26,10 +26,9 @@
 // What a weighted value loses in bfloat16 goes along as further bfloat16 parts: the
 // states that are kept and joined are float32 and have to be near float32's accuracy
 // after any number of chunks (three parts of a value: 2^-27 of it; two parts left
-// states 2e-6 off).  Scores, and states where rows of large calls read them, are
-// rounded once: they end in an output that is rounded alike.  FINE: those states in
-// two parts, which brings outputs from 2.3e-3 to 1.8e-3 of their norm and takes large
-// calls 10 to 15 % more time (16384 ragged rows of 16 heads of 128: 117 and 132 us).
+// states 2e-6 off).  Scores, and states and values where they end in an output, enter as
+// two parts each, which leaves 2^-16 of a term: outputs are off by their own rounding,
+// 1.7e-3 of their norm (scores and states rounded once: 2.3e-3).
 #include "cross_fast.h"
 #include "decay_device.h"
 #include "decay_launch.h"
@@ -39,7 +38,6 @@ namespace {
 
 constexpr int C = 32;         // tokens of a chunk
 constexpr double kLag = 24.0;  // of A, in base 2
-constexpr int64_t kFineRows = 65536;  // rows times key/value heads of a call, 8 chunks a CU
 
 // Byte offset of row r in a tile of PITCH-byte rows; position p of a row holds
 // the 16-byte piece p ^ turn(r).  Reads of a row per lane (16 lanes at a time)
@@ -175,7 +173,7 @@ __device__ __forceinline__ double scan32(double v, double* all) {
 // leave in the next one in whole rows of the block's columns and past the caches
 // (16384 ragged rows of 16 heads of 128: 74 us; 64 bytes of a row at a time 79,
 // and past the caches 101).
-template <int KP, int NW, int MODE, bool FINE>
+template <int KP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
   constexpr bool OUT = MODE == DECAY_OUTPUTS;
@@ -392,18 +390,17 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         for (int i = 0; i < 16; ++i) p[i] = o[i] = 0.f;
 #pragma unroll
         for (int x = 0; x < STEPS; ++x) {
-          constexpr int PARTS = FINE ? 2 : 1;
-          u32x4 sf[PARTS];
+          u32x4 sf[2];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint32_t part2[PARTS];
+            uint32_t part2[2];
             split(s[x / 2][8 * (x & 1) + 2 * i], s[x / 2][8 * (x & 1) + 2 * i + 1], part2);
 #pragma unroll
-            for (int y = 0; y < PARTS; ++y) sf[y][i] = part2[y];
+            for (int y = 0; y < 2; ++y) sf[y][i] = part2[y];
           }
           Tile<MAFAT_BF16>::mul(p, kf[x % AHEAD], qf[x % AHEAD]);
 #pragma unroll
-          for (int y = 0; y < PARTS; ++y) Tile<MAFAT_BF16>::mul(o, sf[y], qf[x % AHEAD]);
+          for (int y = 0; y < 2; ++y) Tile<MAFAT_BF16>::mul(o, sf[y], qf[x % AHEAD]);
           if (x + AHEAD < STEPS) {
             fragment(x + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
@@ -440,11 +437,11 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
             for (int y = 0; y < 3; ++y) vp3[y][u][2 * i + x] = part3[y];
           }
         }
-      u32x4 p0, p1;  // scores, masked
+      u32x4 ps[2][2];  // the scores' parts, of tokens 0 .. 15 and 16 .. 31, masked
       if constexpr (OUT) {
         if (steep) {
-          // c_i and c_j as float32: off by 2^-24 of their size, at most 6400, far
-          // below the scores' rounding
+          // (c_i and c_j as float32 are off by 2^-24 of their size, at most 6400: less than
+          // float32's own sums of as many terms)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + table_here);
@@ -455,10 +452,14 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
           for (int i = 0; i < 16; ++i) o[i] *= e_here;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p0[i] = pack_bf16(p[2 * i], p[2 * i + 1]) & below[i];
-          p1[i] = pack_bf16(p[8 + 2 * i], p[8 + 2 * i + 1]) & below[4 + i];
-        }
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t part2[2];
+            split(p[8 * u + 2 * i], p[8 * u + 2 * i + 1], part2);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) ps[y][u][i] = part2[y] & below[4 * u + i];
+          }
       }
       if (g + 1 == heads) {  // the state after the chunk
         if (steep) times(all);
@@ -485,23 +486,22 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         }
         if (!odd) {
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            Tile<MAFAT_BF16>::mul(o, vp3[y][0], p0);
-            Tile<MAFAT_BF16>::mul(o, vp3[y][1], p1);
-          }
+          for (int y = 0; y < 3; ++y)  // all products of parts but the smallest
+#pragma unroll
+            for (int u = 0; u < 2; ++u) Tile<MAFAT_BF16>::mul(o, vp3[y & 1][u], ps[y >> 1][u]);
         } else {
           // A later token's value must not reach a row, not even times zero: token by token.
 #pragma unroll 1
-          for (int j = 0; j < 2 * C; ++j) {
-            const bool second = j & 16, low = j >= C;
+          for (int j = 0; j < 3 * C; ++j) {
+            const bool second = j & 16, v_low = j / C == 1, p_low = j / C == 2;
             const int token = j & (C - 1);
             u32x4 one, pj;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const bool mine = h == ((j >> 2) & 1) && i == 2 * ((j >> 3) & 1) + ((j >> 1) & 1);
-              const uint32_t v = low ? (second ? vp3[1][1][i] : vp3[1][0][i]) : (second ? vp3[0][1][i] : vp3[0][0][i]);
+              const uint32_t v = v_low ? (second ? vp3[1][1][i] : vp3[1][0][i]) : (second ? vp3[0][1][i] : vp3[0][0][i]);
               one[i] = mine ? v & ((j & 1) ? 0xffff0000u : 0xffffu) : 0u;
-              pj[i] = second ? p1[i] : p0[i];
+              pj[i] = p_low ? (second ? ps[1][1][i] : ps[1][0][i]) : (second ? ps[0][1][i] : ps[0][0][i]);
             }
             f32x16 with = o;
             Tile<MAFAT_BF16>::mul(with, one, pj);
@@ -553,20 +553,20 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
     a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
 }
 
-template <int KP, int NW, int MODE, bool FINE>
+template <int KP, int NW, int MODE>
 hipError_t launch(DecayArgs a, hipStream_t stream) {
   a.slices = (a.value_dim + 32 * NW - 1) / (32 * NW);
   return for_decay_blocks(a, [&](const DecayArgs& p, unsigned n) {
-    hipLaunchKernelGGL((decay_chunk_kernel<KP, NW, MODE, FINE>), dim3(n), dim3(64 * NW), 0, stream, p);
+    hipLaunchKernelGGL((decay_chunk_kernel<KP, NW, MODE>), dim3(n), dim3(64 * NW), 0, stream, p);
   });
 }
 
-template <int MODE, bool FINE>
+template <int MODE>
 hipError_t launch_mode(const DecayArgs& a, hipStream_t stream) {
   const bool few = a.value_dim <= 64;
-  if (a.key_dim <= 64) return few ? launch<64, 2, MODE, FINE>(a, stream) : launch<64, 4, MODE, FINE>(a, stream);
-  if (a.key_dim <= 128) return few ? launch<128, 2, MODE, FINE>(a, stream) : launch<128, 4, MODE, FINE>(a, stream);
-  return few ? launch<256, 2, MODE, FINE>(a, stream) : launch<256, 4, MODE, FINE>(a, stream);
+  if (a.key_dim <= 64) return few ? launch<64, 2, MODE>(a, stream) : launch<64, 4, MODE>(a, stream);
+  if (a.key_dim <= 128) return few ? launch<128, 2, MODE>(a, stream) : launch<128, 4, MODE>(a, stream);
+  return few ? launch<256, 2, MODE>(a, stream) : launch<256, 4, MODE>(a, stream);
 }
 
 }  // namespace
@@ -582,10 +582,7 @@ bool decay_bf16_fits(const DecayArgs& a) {
 }
 
 hipError_t launch_decay_bf16(int mode, const DecayArgs& a, hipStream_t stream) {
-  if (mode == DECAY_ADDS) return launch_mode<DECAY_ADDS, false>(a, stream);
-  // Calls of a few chunks a CU wait for launches and memory, not for a second part of the states.
-  if (static_cast<int64_t>(a.rows) * a.kv_heads <= kFineRows) return launch_mode<DECAY_OUTPUTS, true>(a, stream);
-  return launch_mode<DECAY_OUTPUTS, false>(a, stream);
+  return mode == DECAY_ADDS ? launch_mode<DECAY_ADDS>(a, stream) : launch_mode<DECAY_OUTPUTS>(a, stream);
 }
 
 }  // namespace mafat
