@@ -38,13 +38,6 @@ __device__ __forceinline__ float gate_of(float g, int silu) {
   return (silu ? g : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
 }
 
-// A row's scale in 8 bits, and what values are multiplied by (see row_scale).
-__device__ __forceinline__ float scale_of(uint32_t most, float* inverse) {
-  const float m = __uint_as_float(most);
-  *inverse = m < 0x1p-100f ? 1.f : 448.f * __builtin_amdgcn_rcpf(m);
-  return m < 0x1p-100f ? 1.f : m * (1.f / 448.f);
-}
-
 // v of the lane that CONTROL names.
 template <int CONTROL, typename T>
 __device__ __forceinline__ T other_lane(T v) {
@@ -258,7 +251,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
         most = MaxBits{}(most, __float_as_uint(h[k][i]) & 0x7fffffffu);
     most = team_join<TEAM>(most, MaxBits{}, lds_max);
     float by;
-    const float y_scale = scale_of(most, &by);
+    const float y_scale = row_scale(most, &by);
     if (t == 0) a.y_scale[row] = y_scale;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
