@@ -18,12 +18,25 @@
 namespace mafat {
 namespace {
 
-// What every thread of a row forms for itself is kept short, since it has eight
-// values of it: reciprocals and roots are the hardware's, within one unit.
-
-// 1 / sqrt(v); the hardware's root takes denormal numbers for zeros.
-__device__ __forceinline__ float inverse_root(float v) {
-  return v < 0x1p-96f ? 0x1p50f * __builtin_amdgcn_rsqf(v * 0x1p100f) : __builtin_amdgcn_rsqf(v);
+// A norm's factor 1 / sqrt(sq / n + eps), each step rounded to nearest as norm.hip's
+// divisions and root are.  Every thread of a row forms it for eight values, so where
+// remainders are exact the steps are estimates (`per` is 1 / n) that one remainder
+// corrects (Markstein), a third of the instructions: 16384 rows of 4096 bfloat16 values
+// take 1.6 % more than with the hardware's estimates alone, and 4 % with divisions.  The
+// last reciprocal's correction misses one root, all ones in its mantissa, which numbers
+// of all ones, the last bit aside, have.
+__device__ __forceinline__ float inverse_root(float sq, int n, float per, float eps) {
+  const float count = static_cast<float>(n);
+  if (sq >= 0x1p-60f && sq <= 0x1p100f) {
+    const float q = sq * per;
+    const float m = fmaf(fmaf(-q, count, sq), per, q) + eps;
+    if (m < 0x1p126f && (__float_as_uint(m) & 0x7ffffe) != 0x7ffffe) {
+      const float y = __builtin_amdgcn_rsqf(m), near = m * y;
+      const float root = fmaf(fmaf(-near, near, m), 0.5f * y, near);
+      return fmaf(fmaf(-root, y, 1.f), y, y);
+    }
+  }
+  return 1.f / sqrtf(sq / count + eps);
 }
 
 // g or 1, times 1 / (1 + e^-g).  -g log2(e) in two parts, the second into the
@@ -165,7 +178,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
 #pragma unroll
         for (int i = 0; i < V; ++i) sq = fmaf(h[k][i], h[k][i], sq);
       sq = team_join<TEAM>(sq, Add{}, lds_a);
-      const float one = inverse_root(fmaf(sq, a.per_col, a.eps));
+      const float one = inverse_root(sq, a.cols, a.per_col, a.eps);
 #pragma unroll
       for (int k = 0; k < NP; ++k) inv[k] = one;
     } else {
@@ -182,7 +195,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
 #pragma unroll
           for (int k = 0; k < NP; ++k) sq[k] += __shfl_xor(sq[k], o, 64);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) inv[k] = inverse_root(fmaf(sq[k], a.per_part, a.eps));
+        for (int k = 0; k < NP; ++k) inv[k] = inverse_root(sq[k], a.part, a.per_part, a.eps);
       } else {
         const int lane = t & 63;
 #pragma unroll
@@ -193,7 +206,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
           for (int i = lane; i < pieces; i += 64) s += lds_part[p * pieces + i];
 #pragma unroll
           for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-          if (lane == 0) lds_inv[p] = inverse_root(fmaf(s, a.per_part, a.eps));
+          if (lane == 0) lds_inv[p] = inverse_root(s, a.part, a.per_part, a.eps);
         }
         __syncthreads();
 #pragma unroll
@@ -235,7 +248,7 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
       for (int i = 0; i < V; ++i)
         sq = fmaf(h[k][i], h[k][i], sq);
     sq = team_join<TEAM>(sq, Add{}, lds_b);
-    const float inv = inverse_root(fmaf(sq, a.per_col, a.eps));
+    const float inv = inverse_root(sq, a.cols, a.per_col, a.eps);
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
@@ -286,7 +299,7 @@ __global__ __launch_bounds__(1024) void block_norm_any_kernel(const BlockArgs a)
       float s = 0.f;
       for (int64_t i = tid; i < a.cols; i += TEAM) s = fmaf(to_f(x[i]), to_f(x[i]), s);
       s = team_reduce<TEAM>(s, Add{}, lds_sum[0]);
-      if (tid == 0) lds_inv[0] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+      if (tid == 0) lds_inv[0] = inverse_root(s, a.part, a.per_part, a.eps);
     } else {
       for (int p = tid >> 6; p < a.groups; p += WAVES) {
         float s = 0.f;
@@ -294,7 +307,7 @@ __global__ __launch_bounds__(1024) void block_norm_any_kernel(const BlockArgs a)
         for (int i = lane; i < a.part; i += 64) s = fmaf(to_f(at[i]), to_f(at[i]), s);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-        if (lane == 0) lds_inv[p] = 1.f / sqrtf(s / static_cast<float>(a.part) + a.eps);
+        if (lane == 0) lds_inv[p] = inverse_root(s, a.part, a.per_part, a.eps);
       }
     }
     __syncthreads();
@@ -318,7 +331,7 @@ __global__ __launch_bounds__(1024) void block_norm_any_kernel(const BlockArgs a)
       if (res) store1(sum + c, h);
       s = fmaf(h, h, s);
     }
-    if (a.before) inv = 1.f / sqrtf(team_reduce<TEAM>(s, Add{}, lds_sum[1]) / static_cast<float>(a.cols) + a.eps);
+    if (a.before) inv = inverse_root(team_reduce<TEAM>(s, Add{}, lds_sum[1]), a.cols, a.per_col, a.eps);
   }
   const auto out_at = [&](int64_t c) {
     const float h = sum_at(c);

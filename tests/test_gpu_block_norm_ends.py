@@ -1,7 +1,8 @@
-"""Norms around a block where float32 ends and where a step's rounding can be told: the largest 8-bit rows.
+"""Norms around a block where float32 ends and where a step's rounding can be told: the largest 8-bit rows, and
+norms whose sums are exact.
 
-Where every sum is exact the result is that of float32's own divisions (correctly rounded, as numpy's are), bit by bit, on
-every kernel."""
+Where every sum is exact the result is that of float32's own divisions and roots (correctly rounded, as numpy's are), bit by
+bit, on every kernel and as add_rms_norm has it."""
 import numpy as np
 import pytest
 
@@ -9,6 +10,12 @@ from gpu_util import require_gpu
 
 # columns of every kernel: parts of a wave, waves, two pieces a thread, rows that are read again
 WIDTHS = [8, 64, 100, 512, 1000, 2048, 4096, 8192, 16384, 40004]
+
+
+def _signs(rows, cols, seed):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(0, 2, (rows, cols), generator=g).float() * 2 - 1
 
 
 @pytest.mark.gpu
@@ -30,3 +37,46 @@ def test_rows_in_8_bits_at_the_ends_of_float32(cols, dtype):
     assert np.array_equal(scale.cpu().numpy(), most / np.float32(448))
     by = torch.from_numpy(np.float32(448) / most)
     assert torch.equal(y.cpu().float(), (x.float() * by[:, None]).to(torch.float8_e4m3fn).float())
+
+
+def _inverse_root(sq, n, eps):
+    """1 / sqrt(sq / n + eps), each step rounded to float32."""
+    return np.float32(1) / np.sqrt(np.float32(sq) / np.float32(n) + np.float32(eps))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_norms_divide_and_take_roots(cols):
+    """Rows of plus and minus one number (powers of two times 1, 3 or 5): their sums of squares are exact in any order."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    sizes = torch.tensor([1.0, 3.0, 5.0, 0.375, 96.0, 2.0 ** -20, 5 * 2.0 ** 30, 0.0])
+    x = _signs(len(sizes), cols, cols) * sizes[:, None]
+    x[:, ::3] = 0  # the mean is not the square
+    sq = (x.double() ** 2).sum(1).numpy()
+    assert (np.float32(sq) == sq).all()
+    for eps in (1e-6, 0.3):
+        want = x * torch.from_numpy(_inverse_root(sq, cols, eps))[:, None]
+        for kw in (dict(after=True, before=False), dict(after=False, before=True)):
+            got = O.block_norm(x.cuda(), eps=eps, out="f32", **kw)[1]
+            assert torch.equal(got.cpu(), want), (kw, (got.cpu() - want).abs().max())
+        assert torch.equal(O.add_rms_norm(x.cuda(), eps=eps, out="f32")[1].cpu(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols, groups", [(64, 8), (4096, 32), (8192, 64), (16384, 128), (96, 4), (960, 5), (9600, 3), (16320, 20),
+                                          (33, 3), (40, 40), (1000, 8), (40000, 10)])
+def test_norms_of_parts_divide_and_take_roots(cols, groups):
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    x = _signs(6, cols, cols) * torch.tensor([1.0, 3.0, 5.0, 0.375, 2.0 ** -20, 5 * 2.0 ** 30])[:, None]
+    x[:, ::5] = 0
+    parts = x.view(6, groups, -1)
+    sq = (parts.double() ** 2).sum(2).numpy()
+    assert (np.float32(sq) == sq).all()
+    for eps in (1e-6, 0.3):
+        inv = torch.from_numpy(_inverse_root(sq, cols // groups, eps))
+        got = O.block_norm(x.cuda(), groups=groups, eps=eps, before=False, out="f32")[1]
+        assert torch.equal(got.cpu(), (parts * inv[..., None]).view(6, cols))
