@@ -39,16 +39,23 @@ __device__ __forceinline__ float inverse_root(float sq, int n, float per, float 
   return 1.f / sqrtf(sq / count + eps);
 }
 
-// g or 1, times 1 / (1 + e^-g).  -g log2(e) in two parts, the second into the
-// exponential as its derivative: within a few units however large g is.
+// g or 1, times 1 / (1 + e^-g), as 2^-64 / (2^-64 + e^-g 2^-64): then neither the
+// exponential nor the reciprocal leaves float32's normal numbers, which the hardware's
+// instructions take, before the result does.  -g log2(e) in two parts, the second into
+// the exponential as its derivative: within a few units down to where the result is
+// zero.  (Below -110 the exponential counts as infinite: a gate times e^-110 is less than
+// the least number.)
 __device__ __forceinline__ float gate_of(float g, int silu) {
-  const float near = g > 104.f ? 104.f : g < -104.f ? -104.f : g;  // (beyond, the exponential is 0 or infinite; NaN stays)
-  const float t = near * -1.44269504f;
-  const float rest = fmaf(near, -1.44269504f, -t) + near * -1.92596299e-8f;
-  float e = __builtin_amdgcn_exp2f(t);
+#pragma clang fp contract(off)  // (t is one rounded product wherever it is used)
+  const float near = __builtin_amdgcn_fmed3f(g, -110.f, 110.f);
+  const float t = near * -1.44269504f, down = t - 64.f;
+  // (what `down` has of t: the sum is exact, as down's last bit is 2^-16 at most)
+  const float rest = fmaf(near, -1.92596299e-8f, fmaf(near, -1.44269504f, -(down + 64.f)));
+  float e = __builtin_amdgcn_exp2f(down);
   e = fmaf(e, rest * 0.693147181f, e);
-  e = t > 127.f ? __builtin_huge_valf() : e;  // (where the correction may be of something infinite)
-  return (silu ? g : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+  e = g >= -110.f ? e : g * -__builtin_huge_valf();  // (NaN stays)
+  const float open = silu ? g : 1.f;
+  return g > 110.f ? open : open * __builtin_amdgcn_rcpf(0x1p-64f + e) * 0x1p-64f;
 }
 
 // v of the lane that CONTROL names.

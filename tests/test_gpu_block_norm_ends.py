@@ -1,5 +1,5 @@
-"""Norms around a block where float32 ends and where a step's rounding can be told: the largest 8-bit rows, and
-norms whose sums are exact.
+"""Norms around a block where float32 ends and where a step's rounding can be told: the largest 8-bit rows, gates that
+nearly close, and norms whose sums are exact.
 
 Where every sum is exact the result is that of float32's own divisions and roots (correctly rounded, as numpy's are), bit by
 bit, on every kernel and as add_rms_norm has it."""
@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 
 from gpu_util import require_gpu
+from test_gpu_block_norm import E
 
 # columns of every kernel: parts of a wave, waves, two pieces a thread, rows that are read again
 WIDTHS = [8, 64, 100, 512, 1000, 2048, 4096, 8192, 16384, 40004]
@@ -80,3 +81,26 @@ def test_norms_of_parts_divide_and_take_roots(cols, groups):
         inv = torch.from_numpy(_inverse_root(sq, cols // groups, eps))
         got = O.block_norm(x.cuda(), groups=groups, eps=eps, before=False, out="f32")[1]
         assert torch.equal(got.cpu(), (parts * inv[..., None]).view(6, cols))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [64, 40004])
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+def test_gates_that_nearly_close(act, cols):
+    """From where the exponential is near float32's end to where the gate is zero: values below 2^-126 are off by half of float32's
+    least step, 2^-149, a factor of 2 for x and a second rounding; the others by 8 units."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    gate = torch.linspace(-120, -60, cols).view(1, cols).cuda()
+    x = torch.full_like(gate, 2.0)
+    _, y, _ = O.block_norm(x, after=False, gate=gate, act=act, before=False, out="f32")
+    g = gate.double()
+    want = 2 * (g if act == "silu" else 1) / (1 + torch.exp(-g))
+    assert ((y.double() - want).abs() <= 16 * E * want.abs() + 2 * 2.0 ** -149).all(), ((y.double() - want) / want).abs().max()
+    far = torch.tensor([[-float("inf"), -1e30, float("nan"), float("inf"), 1e30, -111.0, -104.0, 3.0]], device="cuda")
+    got = O.block_norm(torch.ones_like(far), after=False, gate=far, act=act, before=False, out="f32")[1]
+    want = (far if act == "silu" else 1) / (1 + torch.exp(-far.double()))
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    fine = ~torch.isnan(want)
+    assert ((got.double() == want) | ((got.double() - want).abs() <= 16 * E * want.abs() + 2.0 ** -149))[fine].all(), (got, want)
