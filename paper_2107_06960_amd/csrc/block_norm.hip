@@ -202,7 +202,8 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void block_norm_kernel(cons
 #pragma unroll
           for (int k = 0; k < NP; ++k) sq[k] += __shfl_xor(sq[k], o, 64);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) inv[k] = inverse_root(sq[k], a.part, a.per_part, a.eps);
+        for (int k = 0; k < NP; ++k)  // (past the row's end there is no part: with an eps of 0 its factor would be infinite)
+          inv[k] = (k * TEAM + t) * V < a.cols ? inverse_root(sq[k], a.part, a.per_part, a.eps) : 0.f;
       } else {
         const int lane = t & 63;
 #pragma unroll

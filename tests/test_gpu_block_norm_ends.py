@@ -1,5 +1,5 @@
 """Norms around a block where float32 ends and where a step's rounding can be told: the largest 8-bit rows, gates that
-nearly close, and norms whose sums are exact.
+nearly close, parts without a floor, and norms whose sums are exact.
 
 Where every sum is exact the result is that of float32's own divisions and roots (correctly rounded, as numpy's are), bit by
 bit, on every kernel and as add_rms_norm has it."""
@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from gpu_util import require_gpu
-from test_gpu_block_norm import E
+from test_gpu_block_norm import E, _check
 
 # columns of every kernel: parts of a wave, waves, two pieces a thread, rows that are read again
 WIDTHS = [8, 64, 100, 512, 1000, 2048, 4096, 8192, 16384, 40004]
@@ -104,3 +104,23 @@ def test_gates_that_nearly_close(act, cols):
     assert torch.equal(torch.isnan(got), torch.isnan(want))
     fine = ~torch.isnan(want)
     assert ((got.double() == want) | ((got.double() - want).abs() <= 16 * E * want.abs() + 2.0 ** -149))[fine].all(), (got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols, groups", [(768, 12), (96, 4), (64, 8), (480, 15), (2560, 20), (5120, 40), (9600, 75), (960, 5), (9600, 3),
+                                          (16320, 20), (33, 3), (1000, 8), (40000, 10), (100, 1), (1000, 1)])
+def test_parts_without_a_floor(cols, groups, dtype):
+    """eps = 0: rows and parts that are not zeros have their norm, whatever their team's threads past the row's end hold."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    g = torch.Generator().manual_seed(cols)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, gate, res = ((torch.randn(5, cols, generator=g) + 0.1).to(dt).cuda() for _ in range(3))
+    for kw in (dict(before=True, out="f8"), dict(before=False, out="f8"), dict(before=True, out=dtype, residual=res, gate=gate)):
+        args = dict(dict(x=x, after=True, after_gain=None, groups=groups, gate=None, act="silu", scale=None, residual=None, before=True,
+                         before_gain=None, eps=0.0, out="f8"), **kw)
+        result = O.block_norm(**args)
+        assert torch.isfinite(result[1].float()).all()
+        _check(args, result)
