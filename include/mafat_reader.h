@@ -267,8 +267,8 @@ typedef struct {
  * requests have more than one row, scores, and states and values where they end in
  * an output, enter products as two bfloat16 parts each, which leave 2^-16 of a
  * term: outputs are off by their own rounding, whatever else is in the call.  The
- * states that are kept have float32's accuracy.  There what a
- * token adds to the state overflows above 2e31, 2^-24 of float32's largest.  Errors:
+ * states that are kept have float32's accuracy, but for 2^-102 of a key that a
+ * value may lose.  Errors:
  * EINVAL (null or misaligned pointer, bad size or stride, rows not divisible
  * without offsets, scale not finite, an output overlapping another tensor),
  * EWORKSPACE, EUNSUPPORTED (dtype, key_dim or value_dim > 256, rows * q_heads or

@@ -15,12 +15,14 @@
 // 16384 ragged rows of 16 heads of 128: 38 us for what segments add, 74 for the
 // outputs; 65536 rows of 8 heads that pairs share: 38 and 96 (4.4 TB/s).
 //
-// The state is kept relative to a factor 2^A: S = 2^A S', A the logarithm of
-// the decays since it was last brought up to date.  With v'_j = 2^(-A - c_j) v_j
+// The state is kept relative to a factor 2^A: S = 2^A S', A between 0 and kLag, less the
+// decays since it was last brought up to date.  With v'_j = 2^(-A - c_j) v_j
 //   y_i = scale 2^(A + c_i) (q_i S' + sum_{j <= i} (q_i . k_j) v'_j),  S' += sum_j k_j v'_j^T
 // so a chunk takes no exponentials but one a token, and no product of the whole
-// state.  S' is multiplied by 2^A and A set to zero when A + c_C would pass
-// -kLag: float32 and bfloat16 have room for the factor.  A chunk that forgets
+// state.  S' is multiplied by 2^(A - kLag) and A set to kLag when A + c_C would pass
+// 0.  So no weight is above 1 and nothing grows on the way: what is finite by the formula
+// is finite here (masked scores times an infinite weighted value would reach earlier
+// rows); terms may lose what is below 2^-126 + kLag instead.  A chunk that forgets
 // more than that by itself takes exponentials of differences, as decay.hip says.
 //
 // What a weighted value loses in bfloat16 goes along as further bfloat16 parts: the
@@ -37,7 +39,7 @@ namespace mafat {
 namespace {
 
 constexpr int C = 32;         // tokens of a chunk
-constexpr double kLag = 24.0;  // of A, in base 2
+constexpr double kLag = 24.0;  // the most that A is
 
 // Byte offset of row r in a tile of PITCH-byte rows; position p of a row holds
 // the 16-byte piece p ^ turn(r).  Reads of a row per lane (16 lanes at a time)
@@ -132,6 +134,14 @@ __device__ __forceinline__ void split(float x, float y, uint32_t (&part)[N]) {
     x -= lower(part[i]);
     y -= upper(part[i]);
   }
+}
+
+// 2^x, its exponent's whole part apart: within float32's rounding for large x too, and
+// with what is left of numbers below the least normal one.
+__device__ __forceinline__ float power2(double x) {
+  const double whole = __builtin_rint(x);
+  // (the maximum is for NaN, which no integer has and the exponential keeps)
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(__builtin_fmax(whole, -1e6)));
 }
 
 // Waits for all loads, also as the compiler counts them: one that it takes for
@@ -308,7 +318,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
     }
   };
   auto times = [&](double log2) {
-    const float by = __builtin_amdgcn_exp2f(static_cast<float>(log2));
+    const float by = power2(log2);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -363,15 +373,15 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
           all = n * one;
         }
         total += all;
-        if (!(lag + all >= -kLag)) {
-          times(lag);
-          lag = 0.0;
-          steep = !(all >= -kLag);
+        if (!(lag + all >= 0.0)) {
+          steep = !(kLag + all >= 0.0);
+          times(steep ? lag : lag - kLag);
+          lag = steep ? 0.0 : kLag;
         }
         c_here = static_cast<float>(ci);
-        e_here = __builtin_amdgcn_exp2f(static_cast<float>(lag + ci));
+        e_here = power2(lag + ci);
         tc[c] = c_here;
-        tw[c] = __builtin_amdgcn_exp2f(static_cast<float>(steep ? all - ci : -lag - ci));
+        tw[c] = power2(steep ? all - ci : -lag - ci);
         const unsigned char* v = sv + kv_slot * VTILE;
         uint32_t bad = 0;
 #pragma unroll
@@ -550,7 +560,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[t][r]), rsrc, static_cast<int>(entry(t, r)), 0, 0);
   }
   if (!OUT && slice == 0 && threadIdx.x == 0)
-    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
+    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = power2(total);
 }
 
 template <int KP, int NW, int MODE>
@@ -572,12 +582,12 @@ hipError_t launch_mode(const DecayArgs& a, hipStream_t stream) {
 }  // namespace
 
 bool decay_bf16_fits(const DecayArgs& a) {
-  // whole pieces, and a segment's extent in 31 bits
+  // whole pieces, a segment's extent in 31 bits, and a scale that has room for 2^kLag
   const int64_t rows = static_cast<int64_t>(a.segment) + C;
   const auto whole = [&](const void* p, int64_t row, int64_t head) {
     return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * (row | head))) & 15) == 0 && rows * row < (int64_t{1} << 30) - 512;
   };
-  return a.key_dim % 8 == 0 && a.value_dim % 8 == 0 && whole(a.q, a.q_row, a.q_head) && whole(a.k, a.k_row, a.k_head) &&
+  return a.key_dim % 8 == 0 && a.value_dim % 8 == 0 && a.scale < 0x1p100f && a.scale > -0x1p100f && whole(a.q, a.q_row, a.q_head) && whole(a.k, a.k_row, a.k_head) &&
          whole(a.v, a.v_row, a.v_head) && (!a.decay_by_row || rows * a.decay_row < (int64_t{1} << 29));
 }
 

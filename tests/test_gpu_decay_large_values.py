@@ -1,0 +1,85 @@
+"""Linear attention with decays where values are large or small: finite tokens do not reach the rows ahead of them, and what is
+finite by the formula is so here.
+
+Bounds as in test_gpu_decay_accuracy.py and test_gpu_decay.py, singly: (dk + n + 64) 2^-24 of the sum of magnitudes, in
+bfloat16 4 * 2^-16 more, and 2^-8 of the value for its own rounding."""
+import pytest
+
+from gpu_util import require_gpu
+from test_gpu_decay import E, _inputs, _norm, _reference
+
+
+def _run(x, scale=None):
+    from paper_2107_06960_amd import operators as O
+    states = x["states"].clone()
+    return O.decay_attention(x["q"], x["k"], x["v"], x["log_decay"], states=states, scale=scale), states
+
+
+def _check(x, scale, got):
+    import torch
+    y, kept = got
+    rows, _, dk = x["q"].shape
+    n = rows // x["states"].shape[0]
+    want, states, size, sizes = _reference(x["q"], x["k"], x["v"], x["log_decay"], x["states"], None,
+                                           list(range(0, rows + 1, n)), scale)
+    bf16 = x["q"].element_size() == 2
+    rel = (dk + n + 64) * E + (4 * 2.0 ** -16 if bf16 else 0)
+    assert torch.isfinite(want).all() and torch.isfinite(y).all() and torch.isfinite(kept).all()
+    # (2^-102: a 2^24th of the least normal number, which terms lose that are kept relative to a factor)
+    assert ((y.double().cpu() - want).abs() <= rel * size + (2.0 ** -8 * want.abs() if bf16 else 0) + 2.0 ** -102).all()
+    assert ((kept.double().cpu() - states).abs() <= rel * sizes + 2.0 ** -102).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rate", [0.1, 0.5, 2.0])
+def test_large_values_of_small_keys(d, rate, dtype):
+    """A value of 1e35 whose key is 1e-10, late in a chunk: rows ahead of it are what they were, those after it finite."""
+    require_gpu()
+    import torch
+    for n, at in ((40, 20), (96, 95), (400, 31), (700, 640)):
+        x = _inputs(n, 2, 1, d, d, dtype, n + d, pool=1, rate=rate)
+        clean, _ = _run(x, 0.1)
+        x["v"][at, 0, 5] = 1e35
+        x["k"][at] *= 1e-10 / x["k"][at].float().abs().max()
+        y, kept = got = _run(x, 0.1)
+        other = torch.ones_like(y, dtype=torch.bool)
+        other[at:] = False
+        assert torch.isfinite(y).all() and torch.isfinite(kept).all()
+        assert _norm((y[other] - clean[other]).double()) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -18) * _norm(clean[other].double())
+        _check(x, 0.1, got)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("by", [1e33, 1e36, 1e-25])
+def test_values_far_from_one(by, dtype):
+    """All values large, states and outputs within float32 all the same; and all of them small."""
+    require_gpu()
+    for n in (70, 600):
+        x = _inputs(n, 2, 2, 64, 64, dtype, n, pool=1, rate=0.2)
+        x["v"] *= by
+        x["k"] *= 0.01
+        x["q"] *= 0.1
+        x["states"] *= by
+        _check(x, 0.125, _run(x, 0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-36, 1e36, -1e-30, 0.0])
+def test_scales_far_from_one(scale, dtype):
+    """Outputs whose size comes back through their scale."""
+    require_gpu()
+    for n in (70, 600):
+        x = _inputs(n, 2, 2, 64, 64, dtype, n, pool=1, rate=0.2)
+        if scale:
+            by = abs(scale) ** -0.9
+            x["v"] *= by
+            x["states"] *= by
+        y, _ = _run(x, scale)
+        want, _, size, _ = _reference(x["q"], x["k"], x["v"], x["log_decay"], x["states"], None, [0, n], scale)
+        bf16 = dtype == "bf16"
+        rel = (64 + n + 64) * E + (4 * 2.0 ** -16 if bf16 else 0)
+        assert ((y.double().cpu() - want).abs() <= rel * size + (2.0 ** -8 * want.abs() if bf16 else 0) + 1e-37).all()
