@@ -180,7 +180,8 @@ typedef struct {
  *   turns      float64 [axes][pairs], contiguous: turns per step, for instance
  *              base^(-i / pairs) / (2 pi)
  *   qy, ky     may be q and k themselves (with their strides); otherwise outputs
- *              may not overlap inputs or each other
+ *              may not overlap inputs or each other.  Tensors of one pair of
+ *              strides may lie between each other in any order
  * t is formed and brought below half a turn in float64, its sine and cosine in
  * float32: far positions keep the accuracy of near ones.  Errors: EINVAL (null
  * or misaligned pointer, negative rows or heads, axes outside 1 .. 4, pairs < 0

@@ -68,5 +68,33 @@ inline Span rows_of_heads(const void* p, int64_t esz, int64_t d, int64_t rows, i
   return extent(p, esz, d, {{rows, row}, {heads, head}});
 }
 
+// `d` values of each of `heads` heads in `rows` rows, strides in elements.
+struct Heads {
+  const void* p;
+  int64_t esz, d, rows, row, heads, head;
+  Span span() const { return rows_of_heads(p, esz, d, rows, row, heads, head); }
+};
+
+// Whether two such tensors share a byte.  Those of one pair of strides may lie
+// between each other in any order (queries, keys and values head by head, say):
+// then heads j - i = m and rows apart by n are D + m head + n row bytes apart, D the
+// tensors' distance.  Others count as `overlap` says.
+inline bool heads_overlap(const Heads& a, const Heads& b) {
+  if (!overlap(a.span(), b.span())) return false;
+  if (a.esz != b.esz || (a.rows > 1 && b.rows > 1 && a.row != b.row) || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return true;
+  const int64_t row = (a.rows > 1 ? a.row : b.row) * a.esz, head = (a.heads > 1 ? a.head : b.head) * a.esz;
+  const int64_t wa = a.d * a.esz, wb = b.d * b.esz;
+  const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  for (int64_t m = 1 - a.heads; m < b.heads; ++m) {
+    const int64_t x = apart + m * head;
+    // rows n with -wb < x + n row < wa, the first of them by a quotient towards minus infinity
+    const int64_t from = -wb - x;
+    int64_t n = (from >= 0 ? from / row : -((row - 1 - from) / row)) + 1;
+    if (n < 1 - a.rows) n = 1 - a.rows;
+    if (n < b.rows && x + n * row < wa) return true;
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace mafat

@@ -85,14 +85,13 @@ extern "C" int mafat_rotary(const mafat_turns* c, const int32_t* positions, cons
     const int64_t esz = static_cast<int64_t>(es);
     const bool q_in = q == qy && (c->rows == 1 || c->q_row == c->qy_row) && (c->q_heads == 1 || c->q_head == c->qy_head);
     const bool k_in = has_k && k == ky && (c->rows == 1 || c->k_row == c->ky_row) && (c->k_heads == 1 || c->k_head == c->ky_head);
-    const Span sq = rows_of_heads(q, esz, d, c->rows, c->q_row, c->q_heads, c->q_head);
-    const Span so = rows_of_heads(qy, esz, d, c->rows, c->qy_row, c->q_heads, c->qy_head);
-    const Span sk = has_k ? rows_of_heads(k, esz, d, c->rows, c->k_row, c->k_heads, c->k_head) : Span{nullptr, 0, 0, 0};
-    const Span sy = has_k ? rows_of_heads(ky, esz, d, c->rows, c->ky_row, c->k_heads, c->ky_head) : Span{nullptr, 0, 0, 0};
+    const Heads hq{q, esz, d, c->rows, c->q_row, c->q_heads, c->q_head}, ho{qy, esz, d, c->rows, c->qy_row, c->q_heads, c->qy_head};
+    const Heads hk{k, esz, d, c->rows, c->k_row, c->k_heads, c->k_head}, hy{ky, esz, d, c->rows, c->ky_row, c->k_heads, c->ky_head};
     const int64_t pn = 4 * c->rows * c->axes, tn = 8 * int64_t{c->axes} * c->pairs;
     const Span sp{positions, 1, pn, pn}, st{c->pairs ? turns : nullptr, 1, tn, tn};
-    if ((!q_in && overlap(so, sq)) || (!k_in && overlap(sy, sk)) || overlap(so, sk) || overlap(sy, sq) || overlap(so, sy) ||
-        overlap(so, sp) || overlap(so, st) || overlap(sy, sp) || overlap(sy, st))
+    if ((!q_in && heads_overlap(ho, hq)) || overlap(ho.span(), sp) || overlap(ho.span(), st) ||
+        (has_k && ((!k_in && heads_overlap(hy, hk)) || heads_overlap(ho, hk) || (!(q_in && k_in) && (heads_overlap(hy, hq) || heads_overlap(ho, hy))) ||
+                   overlap(hy.span(), sp) || overlap(hy.span(), st))))
       return fail(MAFAT_EINVAL, "an output overlaps another tensor without being its own input");
     RotaryArgs a{};
     a.positions = positions;
@@ -198,16 +197,17 @@ extern "C" int mafat_decay_attention(const mafat_decay* c, const void* q, const 
     const int64_t esz = static_cast<int64_t>(es), size = int64_t{c->kv_heads} * c->key_dim * c->value_dim;
     const int64_t dn = 4 * (c->decay_by_row ? (c->rows - 1) * c->decay_row + c->kv_heads : int64_t{c->kv_heads});
     const int64_t on = 4 * (c->requests + int64_t{1}), sn = 4 * int64_t{c->requests};
-    const Span ins[] = {rows_of_heads(q, esz, c->key_dim, c->rows, c->q_row, c->q_heads, c->q_head),
-                        rows_of_heads(k, esz, c->key_dim, c->rows, c->k_row, c->kv_heads, c->k_head),
-                        rows_of_heads(v, esz, c->value_dim, c->rows, c->v_row, c->kv_heads, c->v_head),
-                        {log_decay, 1, dn, dn}, {offsets, 1, on, on}, {slots, 1, sn, sn}};
-    const Span outs[] = {rows_of_heads(y, esz, c->value_dim, c->rows, c->y_row, c->q_heads, c->y_head),
-                         {c->slots > 0 ? states : nullptr, c->slots, 4 * size, 4 * c->state_slot},
+    const Heads heads[] = {{q, esz, c->key_dim, c->rows, c->q_row, c->q_heads, c->q_head},
+                           {k, esz, c->key_dim, c->rows, c->k_row, c->kv_heads, c->k_head},
+                           {v, esz, c->value_dim, c->rows, c->v_row, c->kv_heads, c->v_head}};
+    const Heads hy{y, esz, c->value_dim, c->rows, c->y_row, c->q_heads, c->y_head};
+    const Span ins[] = {heads[0].span(), heads[1].span(), heads[2].span(), {log_decay, 1, dn, dn}, {offsets, 1, on, on}, {slots, 1, sn, sn}};
+    const Span outs[] = {hy.span(), {c->slots > 0 ? states : nullptr, c->slots, 4 * size, 4 * c->state_slot},
                          {need ? workspace : nullptr, 1, static_cast<int64_t>(need), static_cast<int64_t>(need)}};
     for (int i = 0; i < 3; ++i) {
-      for (const Span& s : ins)
-        if (overlap(outs[i], s)) return fail(MAFAT_EINVAL, "y, the states or the workspace overlaps an input");
+      for (int j = 0; j < 6; ++j)
+        if (i == 0 && j < 3 ? heads_overlap(hy, heads[j]) : overlap(outs[i], ins[j]))
+          return fail(MAFAT_EINVAL, "y, the states or the workspace overlaps an input");
       for (int j = 0; j < i; ++j)
         if (overlap(outs[i], outs[j])) return fail(MAFAT_EINVAL, "y, the states and the workspace overlap");
     }
