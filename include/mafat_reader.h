@@ -186,7 +186,7 @@ typedef struct {
  * float32: far positions keep the accuracy of near ones.  Errors: EINVAL (null
  * or misaligned pointer, negative rows or heads, axes outside 1 .. 4, pairs < 0
  * or 2 * pairs > head_dim, stride below head_dim, magnitude not finite,
- * overlap), EUNSUPPORTED (dtype, head_dim > 1024, rows of 2^31 or more, more
+ * overlap, also of an output's own heads), EUNSUPPORTED (dtype, head_dim > 1024, rows of 2^31 or more, more
  * than 65535 heads, strides of 2^31 or more), EHIP. */
 int mafat_rotary(const mafat_turns* c, const int32_t* positions, const double* turns, const void* q, const void* k,
                  void* qy, void* ky, void* stream);
@@ -271,7 +271,8 @@ typedef struct {
  * states that are kept have float32's accuracy, but for 2^-102 of a key that a
  * value may lose.  Errors:
  * EINVAL (null or misaligned pointer, bad size or stride, rows not divisible
- * without offsets, scale not finite, an output overlapping another tensor),
+ * without offsets, scale not finite, an output overlapping another tensor, or y's
+ * heads each other),
  * EWORKSPACE, EUNSUPPORTED (dtype, key_dim or value_dim > 256, rows * q_heads or
  * requests * kv_heads of 2^31 or more, more than 65535 kv_heads, strides of 2^31
  * bytes or more), EHIP. */

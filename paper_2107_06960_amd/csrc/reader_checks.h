@@ -96,5 +96,16 @@ inline bool heads_overlap(const Heads& a, const Heads& b) {
   return false;
 }
 
+// Whether one such tensor, which is written, has a byte twice.
+inline bool heads_collide(const Heads& a) {
+  const int64_t in_row = (a.heads - 1) * a.head + a.d, in_head = (a.rows - 1) * a.row + a.d;
+  if (!a.p || a.rows <= 1 || a.heads <= 1 || a.row >= in_row || a.head >= in_head) return false;
+  for (int64_t m = 1; m < a.heads; ++m) {  // m heads up and n rows down
+    const int64_t x = m * a.head, n = x / a.row;
+    if ((n < a.rows && x - n * a.row < a.d) || (n + 1 < a.rows && (n + 1) * a.row - x < a.d)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace mafat

@@ -93,6 +93,7 @@ extern "C" int mafat_rotary(const mafat_turns* c, const int32_t* positions, cons
         (has_k && ((!k_in && heads_overlap(hy, hk)) || heads_overlap(ho, hk) || (!(q_in && k_in) && (heads_overlap(hy, hq) || heads_overlap(ho, hy))) ||
                    overlap(hy.span(), sp) || overlap(hy.span(), st))))
       return fail(MAFAT_EINVAL, "an output overlaps another tensor without being its own input");
+    if (heads_collide(ho) || (has_k && heads_collide(hy))) return fail(MAFAT_EINVAL, "heads of an output overlap each other");
     RotaryArgs a{};
     a.positions = positions;
     a.turns = turns;
@@ -211,6 +212,7 @@ extern "C" int mafat_decay_attention(const mafat_decay* c, const void* q, const 
       for (int j = 0; j < i; ++j)
         if (overlap(outs[i], outs[j])) return fail(MAFAT_EINVAL, "y, the states and the workspace overlap");
     }
+    if (heads_collide(hy)) return fail(MAFAT_EINVAL, "heads of y overlap each other");
     DecayArgs a{};
     const DecayPlan p = plan_decay(*c);
     a.q = q; a.k = k; a.v = v; a.log_decay = log_decay; a.offsets = offsets;

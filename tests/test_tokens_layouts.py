@@ -1,5 +1,5 @@
 """CPU tests: which layouts the C entries of the operators among a request's tokens refuse because an output would write what
-another tensor holds (pointers below are never followed: every call is refused)."""
+another tensor, or another of its own heads, holds (pointers below are never followed: every call is refused)."""
 import pytest
 
 from paper_2107_06960_amd import mafat as M
@@ -25,7 +25,17 @@ def test_rotary_refuses_keys_in_the_queries_way(shape, call):
     assert _rotary(shape, call) == M.MAFAT_EINVAL and b"overlaps another tensor" in M.lib().mafat_last_error()
 
 
+@pytest.mark.parametrize("shape, call", [
+    # rows of two heads a head apart; rows half a head into the next ones; three heads up are two rows down
+    (dict(qy_row=64, qy_head=64), {}), (dict(ky_row=96, ky_head=64), {}), (dict(qy_row=192, qy_head=128), {}),
+    (dict(q_row=64, qy_row=64, q_head=64, qy_head=64), dict(qy=C)),
+])
+def test_rotary_refuses_outputs_in_their_own_way(shape, call):
+    assert _rotary(shape, call) == M.MAFAT_EINVAL and b"overlap each other" in M.lib().mafat_last_error()
+
+
 @pytest.mark.parametrize("shape, call, why", [
+    (dict(y_row=32, y_head=32), {}, b"overlap each other"), (dict(y_row=96, y_head=64), {}, b"overlap each other"),
     # y between the queries' heads, and half a head off
     (dict(q_row=4 * 96, q_head=96, y_row=4 * 96, y_head=96), dict(y=A + 2 * 48), b"overlaps an input"),
     (dict(v_row=128, v_head=64, y_row=128, y_head=64, q_heads=2), dict(y=C + 2 * 64), b"overlaps an input"),
