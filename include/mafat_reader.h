@@ -274,8 +274,8 @@ typedef struct {
  * without offsets, scale not finite, an output overlapping another tensor, or y's
  * heads each other),
  * EWORKSPACE, EUNSUPPORTED (dtype, key_dim or value_dim > 256, rows * q_heads or
- * requests * kv_heads of 2^31 or more, more than 65535 kv_heads, strides of 2^31
- * bytes or more), EHIP. */
+ * requests * kv_heads of 2^31 or more, or segments of long requests that make it so,
+ * more than 65535 kv_heads, strides of 2^31 bytes or more), EHIP. */
 int mafat_decay_workspace(const mafat_decay* c, size_t* bytes);
 int mafat_decay_attention(const mafat_decay* c, const void* q, const void* k, const void* v, const float* log_decay,
                           const int32_t* offsets, float* states, const int32_t* slots, void* y, void* workspace,

@@ -41,7 +41,8 @@ int check_decay(const mafat_decay* c, size_t* bytes) {
   *bytes = 0;
   if (p.split) {
     const int64_t states = p.segments * c->kv_heads;
-    // (fewer than 2^31 * 2 states of 2^16 floats and a factor)
+    if (states >= kMax31) return fail(MAFAT_EUNSUPPORTED, "2^31 or more segments of requests and heads");
+    // (states of 2^16 floats and a factor at most)
     *bytes = (static_cast<size_t>(states) * static_cast<size_t>(k * v + 1) * 4 + 255) & ~size_t{255};
   }
   return MAFAT_OK;
