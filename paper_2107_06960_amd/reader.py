@@ -111,14 +111,17 @@ class Reader:
         """tokens: bfloat16 [rows, width], as y has to be, frame by frame; q_offsets: int32 [frames + 1], the frames' rows (None: as many
         each); row_adapter: int32 [rows], the adapter of each row's request, for layers that have adapters (None: without
         them).  For layers that mix: positions: int32 [rows], of the tokens in their requests; offsets: int32 [requests + 1],
-        the requests' rows (None: as many each); memory: what memory() gives, updated in place (None: every request starts
-        without one, and none is kept); slots: int32 [requests], each request's place in it (None: request i has place i).
+        the requests' rows (None: as many each, of as many requests as slots or else memory has places, which have to be given
+        then); memory: what memory() gives, updated in place (None: every request starts without one, and none is kept); slots:
+        int32 [requests], each request's place in it (None: request i has place i).
         Returns the normed rows."""
         if row_adapter is not None and not any(p[i]["adapters"] for p in self.params["layers"] for i in ("q", "o")):
             raise ValueError("row_adapter names adapters, but no layer has any")
         mixes = any("mix" in p for p in self.params["layers"])
         if mixes and (positions is None or not self.mix_heads):
             raise ValueError("layers that mix need positions, and a reader with mix_heads and mix_dim")
+        if mixes and offsets is None and memory is None:
+            raise ValueError("layers that mix need offsets, or a memory, to tell the requests' rows apart")
         if not mixes and any(t is not None for t in (positions, offsets, memory, slots)):
             raise ValueError("positions, offsets, memory and slots are for layers that mix, but no layer does")
         k, v = self.states(y)
