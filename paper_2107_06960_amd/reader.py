@@ -74,7 +74,9 @@ class Reader:
 
     def __init__(self, params, q_heads, kv_heads, head_dim, eps=1e-6, mix_heads=0, mix_dim=0):
         self.params, self.q_heads, self.kv_heads, self.head_dim, self.eps = params, q_heads, kv_heads, head_dim, eps
-        self.mix_heads, self.mix_dim, self._turns = mix_heads, mix_dim, {}
+        self.mix_heads, self.mix_dim = mix_heads, mix_dim
+        # Formed on the host and there when this returns: a run may be recorded by a graph, or be on any stream.
+        self.turns = O.rotary_turns(mix_dim // 2, device="cpu").to(params["gain"].device) if mix_heads else None
 
     def states(self, y):
         """Keys and values, [frames, positions, kv_heads, head_dim] each, in a network's output [frames, h, w, channels]."""
@@ -88,18 +90,13 @@ class Reader:
         """Empty memories of `slots` requests for layers that mix: float32 [layers, slots, mix_heads, mix_dim, mix_dim]."""
         return torch.zeros(len(self.params["layers"]), slots, self.mix_heads, self.mix_dim, self.mix_dim, device=device)
 
-    def _turns_on(self, device):
-        if device not in self._turns:  # once for a device
-            self._turns[device] = O.rotary_turns(self.mix_dim // 2, device=device)
-        return self._turns[device]
-
     def _mix(self, p, h, x, scale, next_gain, positions, offsets, states, slots):
         """The sum after the tokens of each request are mixed, and its norm in 8 bits with `next_gain`."""
         rows, heads, dim = h.shape[0], self.mix_heads, self.mix_dim
         n = heads * dim
         all_ = O.linear8(x, scale, p["qkvg"]["w"], p["qkvg"]["scale"])
         q, k, v = (all_[:, i * n:(i + 1) * n].view(rows, heads, dim) for i in range(3))
-        O.rotary(q, positions, self._turns_on(h.device), k=k, in_place=True)
+        O.rotary(q, positions, self.turns, k=k, in_place=True)
         o = O.decay_attention(q, k, v, p["log_decay"], states=states, slots=slots, offsets=offsets)
         _, x, scale = O.block_norm(o.view(rows, n), after_gain=p["o_gain"], groups=heads, gate=all_[:, 3 * n:], before=False,
                                    eps=self.eps)
