@@ -95,6 +95,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _recording = torch.is_grad_enabled
+_changed = torch.autograd.graph.increment_version  # for tensors that are written in place, through their addresses
 _DENSE = torch.contiguous_format  # (empty_like takes a third less time than empty)
 
 
@@ -420,6 +421,8 @@ def rotary(q, positions, turns, k=None, interleaved=False, magnitude=1.0, in_pla
         qy = torch.empty_like(q, memory_format=_DENSE)
         ky = None if k is None else torch.empty_like(k, memory_format=_DENSE)
     _call("mafat_rotary", dev.index, ref, positions.data_ptr(), turns.data_ptr(), q.data_ptr(), _ptr(k), qy.data_ptr(), _ptr(ky))
+    if in_place:
+        _changed(q if k is None else (q, k))
     return qy, ky
 
 
@@ -562,6 +565,8 @@ def decay_attention(q, k, v, log_decay, states=None, slots=None, offsets=None, s
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call("mafat_decay_attention", dev.index, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), offsets_at,
           states_at, slots_at, y.data_ptr(), _ptr(ws), need)
+    if states is not None:
+        _changed(states)
     return y
 
 
