@@ -6,7 +6,7 @@ maps that a ``mafat.Network`` leaves on the device.
 ``cross_attention``, ``rotary``, ``decay_attention`` and ``block_norm`` take torch tensors on the GPU, check them, allocate
 what they return and run on the current stream of the tensors' device.  There is no fallback: every step
 runs in the library's HIP kernels.  They are forward only: a tensor that requires a gradient is refused while gradients are
-recorded (call under torch.no_grad(), or pass it detached).
+recorded (call under torch.no_grad(), or pass it detached), and so is one with a tangent of forward-mode differentiation.
 """
 from __future__ import annotations
 
@@ -15,6 +15,7 @@ import functools
 import math
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import mafat as M
 
@@ -125,6 +126,17 @@ def _refuse(text):
 
 def _wants_grad(t):
     return t is not None and t.requires_grad
+
+
+def _in_forward_mode():
+    return getattr(_forward, "_current_level", 0) >= 0
+
+
+def _no_tangents(*tensors):
+    """Refuses tangents of forward mode, which `requires_grad` does not tell of."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and _forward.unpack_dual(t).tangent is not None:
+            _forward_only()
 
 
 def _forward_only():
@@ -239,6 +251,8 @@ def add_rms_norm(x, gain=None, residual=None, eps=1e-6, out="f8"):
         _refuse("x must be a float32 or bfloat16 matrix on the GPU")
     if _recording() and (x.requires_grad or _wants_grad(gain) or _wants_grad(residual)):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(x, gain, residual)
     if to is None:
         _refuse(f"out must be one of {sorted(_NAMES)}, not {out!r}")
     rows, cols = x.shape
@@ -276,6 +290,8 @@ def linear8(x, x_scale, w, w_scale, bias=None, adapters=None, row_adapter=None):
     if _recording() and (x.requires_grad or w.requires_grad or _wants_grad(x_scale) or _wants_grad(w_scale) or
                          _wants_grad(bias) or (adapters is not None and any(map(_wants_grad, adapters)))):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(x, w, x_scale, w_scale, bias, *(adapters or ()))
     rows, k = x.shape
     n, dev = w.shape[0], x.device
     if k < 1 or n < 1:
@@ -326,6 +342,8 @@ def cross_attention(q, k, v, q_offsets=None, k_lengths=None, key_mask=None, row_
         _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
     if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or getattr(scale, "requires_grad", False)):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(q, k, v, scale)
     rows, hq, d = q.shape
     dev, shape = q.device, k.shape
     if k.dim() != 4 or shape != v.shape or shape[3] != d or k.dtype is not dt or v.dtype is not dt or k.device != dev or \
@@ -400,6 +418,8 @@ def rotary(q, positions, turns, k=None, interleaved=False, magnitude=1.0, in_pla
         _refuse("q must be a float32 or bfloat16 tensor [rows, heads, d] on the GPU")
     if _recording() and (q.requires_grad or _wants_grad(k) or turns.requires_grad or getattr(magnitude, "requires_grad", False)):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(q, k, turns, magnitude)
     rows, hq, d = q.shape
     dev, hk, ks = q.device, 0, None
     if k is not None:
@@ -464,6 +484,8 @@ def block_norm(x, after=True, after_gain=None, groups=1, gate=None, act="silu", 
     if _recording() and (x.requires_grad or _wants_grad(after_gain) or _wants_grad(gate) or _wants_grad(scale) or
                          _wants_grad(residual) or _wants_grad(before_gain)):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(x, after_gain, gate, scale, residual, before_gain)
     if to is None:
         _refuse(f"out must be one of {sorted(_NAMES)}, not {out!r}")
     if act != "silu" and act != "sigmoid":
@@ -524,6 +546,8 @@ def decay_attention(q, k, v, log_decay, states=None, slots=None, offsets=None, s
     if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
                          _wants_grad(states) or getattr(scale, "requires_grad", False)):
         _forward_only()
+    if _in_forward_mode():
+        _no_tangents(q, k, v, log_decay, states, scale)
     rows, hq, dk = q.shape
     dev = q.device
     if k.dim() != 3 or k.dtype is not dt or k.device != dev or k.shape[0] != rows or k.shape[2] != dk:
