@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
     const int64_t row = first + t;
     const T* kp = static_cast<const T*>(a.k) + row * a.k_row + kv * a.k_head;
     const f32x4 v = load4<T>(static_cast<const T*>(a.v) + row * a.v_row + kv * a.v_head + c, nc);
-    const float g = __builtin_amdgcn_exp2f(decay_log2(a.log_decay[(a.decay_by_row ? row * a.decay_row : 0) + kv]));
+    const float g = power2(decay_log2(a.log_decay[(a.decay_by_row ? row * a.decay_row : 0) + kv]));
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       const int r = r0 + 16 * i;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int i = 16 * ti + 4 * h4 + r;
-            const float w = __builtin_amdgcn_exp2f(static_cast<float>(sc[i] - sc[j]));
+            const float w = power2(static_cast<float>(sc[i] - sc[j]));
             sp[i * PP + j] = j <= i ? p[r] * w : 0.f;
           }
         }
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[ti][r] *= __builtin_amdgcn_exp2f(static_cast<float>(sc[16 * ti + 4 * h4 + r]));
+          for (int r = 0; r < 4; ++r) o[ti][r] *= power2(static_cast<float>(sc[16 * ti + 4 * h4 + r]));
         __syncthreads();
         if (odd) {  // a later token's value must not reach a row, not even times zero
 #pragma unroll
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
     }
     // the state after the chunk
     total += sc[C - 1];
-    const float down = __builtin_amdgcn_exp2f(static_cast<float>(sc[C - 1]));
+    const float down = power2(static_cast<float>(sc[C - 1]));
 #pragma unroll
     for (int i = 0; i < KT; ++i) s[i] *= down;
 #pragma unroll
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int j = 16 * t + 4 * h4 + r;
-        const float v = sv[j * VP + 16 * wave + l16] * __builtin_amdgcn_exp2f(static_cast<float>(sc[C - 1] - sc[j]));
+        const float v = sv[j * VP + 16 * wave + l16] * power2(static_cast<float>(sc[C - 1] - sc[j]));
 #pragma unroll
         for (int i = 0; i < KT; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(sk[j * KP + 16 * i + l16], v, s[i], 0, 0, 0);
       }
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
       }
   }
   if (MODE == DECAY_ADDS && slice == 0 && tid == 0)
-    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = __builtin_amdgcn_exp2f(static_cast<float>(total));
+    a.factor[static_cast<int64_t>(b) * a.kv_heads + kv] = power2(total);
 }
 
 // What segments add -> what they start from, for requests of several segments.

@@ -136,14 +136,6 @@ __device__ __forceinline__ void split(float x, float y, uint32_t (&part)[N]) {
   }
 }
 
-// 2^x, its exponent's whole part apart: within float32's rounding for large x too, and
-// with what is left of numbers below the least normal one.
-__device__ __forceinline__ float power2(double x) {
-  const double whole = __builtin_rint(x);
-  // (the maximum is for NaN, which no integer has and the exponential keeps)
-  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(__builtin_fmax(whole, -1e6)));
-}
-
 // Waits for all loads, also as the compiler counts them: one that it takes for
 // pending in a loop would have it wait there for the loads into LDS too.
 __device__ __forceinline__ void wait_loads() {
@@ -456,7 +448,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
           for (int i = 0; i < 4; ++i) {
             const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + table_here);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p[4 * i + x] *= __builtin_amdgcn_exp2f(c_here - cj[x]);
+            for (int x = 0; x < 4; ++x) p[4 * i + x] *= power2(c_here - cj[x]);
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] *= e_here;

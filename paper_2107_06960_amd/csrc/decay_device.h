@@ -19,6 +19,17 @@ __device__ __forceinline__ float decay_log2(float log_decay) {
   return static_cast<float>(static_cast<double>(l) * kLog2e);
 }
 
+// 2^x, its exponent's whole part apart: within float32's rounding for large x too, and
+// with what is left of numbers below the least normal one, which large states and
+// scores bring back.
+template <typename F>
+__device__ __forceinline__ float power2(F x) {
+  const F whole = __builtin_elementwise_rint(x);
+  // (the maximum is for NaN, which no integer has and the exponential keeps)
+  const int by = static_cast<int>(__builtin_elementwise_max(whole, static_cast<F>(-1e6)));
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), by);
+}
+
 // Rows of request i: first and number.
 __device__ __forceinline__ void rows_of(const DecayArgs& a, int i, int* first, int* n) {
   if (!a.offsets) {

@@ -83,3 +83,17 @@ def test_scales_far_from_one(scale, dtype):
         bf16 = dtype == "bf16"
         rel = (64 + n + 64) * E + (4 * 2.0 ** -16 if bf16 else 0)
         assert ((y.double().cpu() - want).abs() <= rel * size + (2.0 ** -8 * want.abs() if bf16 else 0) + 1e-37).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 2, 40, 600])
+def test_factors_below_the_least_normal_number(n, dtype):
+    """A decay of 2^-128 leaves something of a large state: the factor has 2^-150 / 2^-128 = 4 units of rounding of its own."""
+    require_gpu()
+    x = _inputs(n, 2, 1, 64, 64, dtype, n, pool=1, rate=0.1)
+    x["states"] *= 3e36
+    x["q"] *= 0.1
+    x["k"] *= 0.01
+    x["log_decay"][0] = -89.0
+    _check(x, 0.125, _run(x, 0.125))
