@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayArgs a) {
 // So the state's tile T is the operand of q S as it stands, if step r of the
 // instruction sums over the keys' entries 16 T + 4 (l / 16) + r.  Bound by these
 // instructions, a tenth of bfloat16's rate: 4131 rows of 16 heads of 128 in float32
-// take 123 us, of 59 in bfloat16 71 (of 56, in decay_bf16.hip, 33).
+// take 126 us, of 59 in bfloat16 73 (of 56, in decay_bf16.hip, 37).
 template <int DT, int KT, int MODE>
 __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
   using T = typename Elt<DT>::T;
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void decay_any_kernel(const DecayArgs a) {
 
 // What segments add -> what they start from, for requests of several segments.
 // A thread takes V entries of a head's state through the segments, with the next
-// AHEAD of them on their way.  (121 segments of 4 heads of 128: 15 us with 32 ahead, 19 with 8.)
+// AHEAD of them on their way.  (121 segments of 4 heads of 128: 15 us at best with 32 ahead, 19 with 8.)
 template <int V, int AHEAD>
 __global__ __launch_bounds__(256) void decay_join_kernel(const DecayArgs a) {
   typedef float fv __attribute__((ext_vector_type(V)));
@@ -466,8 +466,8 @@ hipError_t launch(const DecayArgs& a, const DecayPlan& p, hipStream_t stream) {
 DecayPlan plan_decay(const mafat_decay& c) {
   DecayPlan p{};
   // One token a request, if they are alike (two where the chunked kernel is the slow one):
-  // a chunk would be nearly empty.  (64 requests, 16 heads of 128: one token each 28.7 us;
-  // two in turn 31, four in a chunk 26.)
+  // a chunk would be nearly empty.  (64 requests, 16 heads of 128: one token each 28.5 us;
+  // two in turn 31, in a chunk 28; four in a chunk 28.)
   // Segments that leave two blocks a CU, all of them at once: one
   // more would make the call take twice as long.  A request adds a segment that is not
   // full.  With that many requests alone, twice their mean length.
@@ -479,7 +479,7 @@ DecayPlan plan_decay(const mafat_decay& c) {
   int64_t len = most > 2 * int64_t{c.requests} ? c.rows / (most - c.requests) : 2 * (c.rows / c.requests);
   // A chunk takes 1 us in decay_bf16.hip, 3 to 7 here, and the two launches more 8: one request of
   // 1024 rows of 8 heads of 64 takes 30, 22 or 18 us in segments of 256, 128 or 64, of 4096 rows
-  // 32, 26 or 29; one of 130 rows 11.5 whole and 18 in two.
+  // 32, 26 or 29; one of 130 rows 11.5 whole and 18 in two (1 more since states enter outputs in two parts).
   const int64_t least = columns == 64 ? 64 : c.rows <= 256 ? 256 : 128;
   len = len < least ? least : len > 8192 ? 8192 : (len + 31) / 32 * 32;  // (extents of a segment are 31 bits wide)
   p.segment = len;

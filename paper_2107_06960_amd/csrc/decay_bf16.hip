@@ -10,10 +10,11 @@
 // Scores come out as the operand that V^T P^T takes, and the state as the one
 // that S_0^T Q^T takes: K^T's rows are read in the order that makes a lane's 8
 // entries those that a 16-byte piece of a query holds (see dk_of).
-// Every wave forms all of the chunk's scores, 8 of its 36 matrix instructions at
+// Every wave forms all of the chunk's scores, 8 of its 54 matrix instructions at
 // key_dim 128, which costs less than a barrier and a pass through LDS.
-// 16384 ragged rows of 16 heads of 128: 38 us for what segments add, 74 for the
-// outputs; 65536 rows of 8 heads that pairs share: 38 and 96 (4.4 TB/s).
+// 16384 ragged rows of 16 heads of 128: 42 us for what segments add, 105 for the
+// outputs; 65536 rows of 8 heads that pairs share: 45 and 161 (medians; 38, 96, 38 and
+// 134 at best).
 //
 // The state is kept relative to a factor 2^A: S = 2^A S', A between 0 and kLag, less the
 // decays since it was last brought up to date.  With v'_j = 2^(-A - c_j) v_j
@@ -30,7 +31,8 @@
 // after any number of chunks (three parts of a value: 2^-27 of it; two parts left
 // states 2e-6 off).  Scores, and states and values where they end in an output, enter as
 // two parts each, which leaves 2^-16 of a term: outputs are off by their own rounding,
-// 1.7e-3 of their norm (scores and states rounded once: 2.3e-3).
+// 1.7e-3 of their norm.  (Scores and states rounded once: 2.3e-3, and 12 to 16 % less
+// time in large calls: 120 us of 140 for 16384 ragged rows of 16 heads of 128.)
 #include "cross_fast.h"
 #include "decay_device.h"
 #include "decay_launch.h"
@@ -173,8 +175,8 @@ __device__ __forceinline__ double scan32(double v, double* all) {
 // Chunks are asked for SLOTS - 1 iterations ahead, an iteration being a chunk and
 // a query head of the group.  An iteration's outputs go through LDS, so that they
 // leave in the next one in whole rows of the block's columns and past the caches
-// (16384 ragged rows of 16 heads of 128: 74 us; 64 bytes of a row at a time 79,
-// and past the caches 101).
+// (16384 ragged rows of 16 heads of 128, with scores and states rounded once: 74 us;
+// 64 bytes of a row at a time 79, and past the caches 101).
 template <int KP, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(const DecayArgs a) {
   constexpr int KPITCH = 2 * KP, VPITCH = 64 * NW, KT = KP / 32, STEPS = KP / 16;
