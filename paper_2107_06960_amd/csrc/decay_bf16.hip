@@ -24,7 +24,8 @@
 // 0.  So no weight is above 1 and nothing grows on the way: what is finite by the formula
 // is finite here (masked scores times an infinite weighted value would reach earlier
 // rows); terms may lose what is below 2^-126 + kLag instead.  A chunk that forgets
-// more than that by itself takes exponentials of differences, as decay.hip says.
+// more than that by itself takes exponentials of differences, as decay.hip says (where a
+// query's product with the state may overflow that the chunk's decays would bring back).
 //
 // What a weighted value loses in bfloat16 goes along as further bfloat16 parts: the
 // states that are kept and joined are float32 and have to be near float32's accuracy
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
   constexpr int KTILE = C * KPITCH, VTILE = C * VPITCH, DTILE = NW * 256;
   constexpr int AHEAD = 4, TAHEAD = KT < 4 ? KT : 4;  // steps and tiles whose fragments are asked for at once
   __shared__ __align__(1024) unsigned char smem[SLOTS * (KTILE + VTILE + DTILE + (OUT ? KTILE : 0)) + (OUT ? 2 * VTILE : 0)];
-  __shared__ __align__(16) float table[NW][2][C];  // of each wave: c_j, and the values' weights
+  __shared__ __align__(16) float table[NW][3][C];  // of each wave: the values' weights, c_j, and what float32 leaves of it
   const int lane = static_cast<int>(threadIdx.x) & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   // (Slices last: workgroups go round the XCDs, and segments that are not there come
@@ -289,8 +290,9 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
     const int j = 8 * (i >> 1) + 4 * h + 2 * (i & 1);
     below[i] = (j <= c ? 0xffffu : 0u) | (j + 1 <= c ? 0xffff0000u : 0u);
   }
-  float* const tc = table[wave][0];
-  float* const tw = table[wave][1];
+  float* const tw = table[wave][0];
+  float* const tc = table[wave][1];
+  float* const tl = table[wave][2];
 
   wait_loads();
   double total = 0.0, lag = 0.0;  // of the segment's decays, in base 2; A
@@ -375,6 +377,7 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
         c_here = static_cast<float>(ci);
         e_here = power2(lag + ci);
         tc[c] = c_here;
+        tl[c] = static_cast<float>(ci - c_here);
         tw[c] = power2(steep ? all - ci : -lag - ci);
         const unsigned char* v = sv + kv_slot * VTILE;
         uint32_t bad = 0;
@@ -444,13 +447,14 @@ __global__ __launch_bounds__(64 * NW, KP > 128 ? 1 : 2) void decay_chunk_kernel(
       u32x4 ps[2][2];  // the scores' parts, of tokens 0 .. 15 and 16 .. 31, masked
       if constexpr (OUT) {
         if (steep) {
-          // (c_i and c_j as float32 are off by 2^-24 of their size, at most 6400: less than
-          // float32's own sums of as many terms)
+          // (c_i and c_j are up to 6400: as float32 alone, 2.6e-4 of a weight would be lost)
+          const float l_here = tl[c];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const f32x4 cj = *reinterpret_cast<const f32x4*>(tc + 8 * i + table_here);
+            const f32x4 lj = *reinterpret_cast<const f32x4*>(tl + 8 * i + table_here);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p[4 * i + x] *= power2(c_here - cj[x]);
+            for (int x = 0; x < 4; ++x) p[4 * i + x] *= power2((c_here - cj[x]) + (l_here - lj[x]));
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] *= e_here;

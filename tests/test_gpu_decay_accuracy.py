@@ -115,3 +115,20 @@ def test_kept_states(d, n, rate):
     err = _norm(kept.double() - states) / _norm(states)
     assert err <= ((3 * n) ** 0.5 + 8) * E, err
     assert torch.isfinite(kept).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_behind_tokens_that_forget_everything(d):
+    """Thirty factors of 2^-200 and then two tokens that nearly cancel: a weight is that of the decays between its tokens, which
+    the sums of the chunk's decays, 6000, would leave 2^-12 of as float32."""
+    require_gpu()
+    import torch
+    from paper_2107_06960_amd import operators as O
+    x = _inputs(32, 32, 32, d, d, "bf16", d, pool=1, rate=1e-3)
+    x["log_decay"][:30] = -138.0
+    x["k"][31], x["v"][31] = x["k"][30], -x["v"][30]
+    want, _, size = _reference(x, [0, 32], 1.0, [0])
+    y = O.decay_attention(x["q"], x["k"], x["v"], x["log_decay"], states=x["states"].clone(), scale=1.0)
+    over = ((y.double() - want).abs() - _half_step(want)).clamp(min=0)
+    assert (over <= ((d + 32 + 64) * E + 4 * 2.0 ** -16) * size).all(), (over / size).max()
